@@ -458,6 +458,126 @@ int ftp_plan_check(ftp_plan* plan, void* workspace, void* stream);
  */
 int ftp_plan_wait_probe(ftp_plan* plan, void* workspace, int limit_us, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators between and behind the stacks
+ *
+ * A network of several plans needs more than their layers: a norm between one plan's output map and the next one's input,
+ * a loss over class labels beside the mean-squared error, and a way to keep the maps between forward and backward pass in
+ * less memory (the paper counts the feature maps as what fills a device, Section 5.2; between plans they are the joints).
+ * The operators below work on arrays [n, c, p]: n samples of c channels of p pixels, pixels side by side -- the NCHW maps of
+ * a plan with p = H W -- or, with p = 1, matrices of n rows of c values.  Statistics, probabilities and alternatives run along c,
+ * so that an array has n p "rows" of c values, and per-row results are arrays [n, p].
+ *
+ * Arrays are DEVICE memory of the type in ftp_dims, each sample dense; `..._stride` is the number of elements from one sample to
+ * the next (0: dense; else at least c p).  Any alignment that the type itself allows is accepted; 16-byte aligned arrays and strides
+ * are the fast ones.  An output array may be the input array it is computed from where the entry says so; otherwise arrays do not
+ * overlap.  Elements between samples are neither read nor written.  Sums, statistics and probabilities are held in fp32; results
+ * of 16 bits are rounded once, to nearest.  Sums are taken in a fixed order: the same call gives the same bits.
+ *
+ * None of these calls allocates, synchronises, needs a plan or keeps anything between calls, and all can be captured in a CUDA
+ * graph; calls on different streams share nothing but what the caller passes to both (a workspace must not be).  They run on the
+ * current device, which has to be the arrays' own.  n = 0 or p = 0 is an empty array: nothing is read, sums over it are 0.
+ * Errors: FTP_ERR_ARG (null or misaligned pointer, c < 1, a negative size, an unknown type or struct_size, a stride below c p, a
+ * workspace too small), FTP_ERR_TOO_LARGE (n, c or p of 2^30 or more, 2^46 values or more,
+ * or beyond a limit named below), FTP_ERR_CUDA.
+ */
+enum { FTP_TYPE_F32 = 0, FTP_TYPE_BF16 = 1, FTP_TYPE_F16 = 2 };
+
+typedef struct {
+    int struct_size;     /* sizeof(ftp_dims) */
+    int type;            /* FTP_TYPE_* of the arrays */
+    long long n, c, p;   /* samples, channels, pixels of a sample */
+} ftp_dims;
+
+/*
+ * Activation checkpoints in 8 bits: a map put away between forward and backward pass in 33 bytes for 32 values.  Every run
+ * (a row of c values if p = 1, else a plane of p pixels) is cut into blocks of 32 consecutive values, the last one padded with
+ * zeros.  A block is 32 signed bytes q and one exponent byte e, 1 <= e <= 249: the values are q 2^(e - 127) with the least e for
+ * which 127 steps reach the block's largest finite magnitude, and q the nearest integer (ties to even), so that a value is off by
+ * at most half a step, 1/127 of the largest magnitude in its block (values of the order of the type's largest, which the step
+ * would round to infinity, by one step).  A power of two makes quotient and product exact: what a checkpoint holds is
+ * defined to the bit.  An infinity or NaN is kept as q = -128 and comes back as NaN, in its own place alone.
+ *   The q bytes of all runs come first, each run padded to a multiple of 32, then the exponent bytes of all blocks.
+ *   ftp_ckpt_bytes  *bytes = the size of a checkpoint (host call).  `ckpt`: device memory, 16-byte aligned.
+ *   ftp_ckpt_save   writes the checkpoint of x.   ftp_ckpt_load  writes the values of a checkpoint to x, in the type of `d`, which
+ *                   need not be the type it was saved in (values beyond an fp16 then become infinite).
+ */
+int ftp_ckpt_bytes(const ftp_dims* d, size_t* bytes);
+int ftp_ckpt_save(const ftp_dims* d, const void* x, long long x_stride, void* ckpt, void* stream);
+int ftp_ckpt_load(const ftp_dims* d, const void* ckpt, void* x, long long x_stride, void* stream);
+
+/*
+ * ftp_backward from a checkpoint: for a network of several plans that keeps of each plan's input only the checkpoint (dims
+ * {n = N, c = C, p = H W} of the plan's input, any type at saving time) and lets the plans share one workspace.  Writes the
+ * checkpoint's values to x (caller's device buffer, fp32, shape of the plan's input), runs ftp_forward on them (without output map)
+ * and ftp_backward: dx and dparams are those of the plan at the values of the checkpoint.  Needs no preceding ftp_forward.
+ * Arguments otherwise as for ftp_backward; dx must not be x.
+ */
+int ftp_backward_ckpt(ftp_plan* plan, const void* ckpt, float* x, const float* dy, const float* params, float* dx, float* dparams,
+                      void* workspace, void* stream);
+
+/*
+ * Channel norm (layer norm over the channels of each row):
+ *   mean = (1/c) sum x,  rstd = 1 / sqrt((1/c) sum (x - mean)^2 + eps),  y = (x - mean) rstd weight + bias.
+ * weight, bias: device, c floats, each may be NULL (1 and 0).  mean, rstd: device, n p floats, each may be NULL; the backward pass needs
+ * them.  eps >= 0 and finite.  y may be x.
+ * ckpt (may be NULL) receives the checkpoint of x, as by ftp_ckpt_save, from the same reading of x.
+ */
+int ftp_norm_forward(const ftp_dims* d, const void* x, long long x_stride, const float* weight, const float* bias, float eps,
+                     void* y, long long y_stride, float* mean, float* rstd, void* ckpt, void* stream);
+
+/*
+ * Backward pass of the channel norm: with hat = (x - mean) rstd and g = dy weight
+ *   dx = rstd (g - (1/c) sum g - hat (1/c) sum g hat),  dweight = sum over all rows of dy hat,  dbias = sum over all rows of dy.
+ * Give exactly one of x and ckpt: with ckpt, x is the values of the checkpoint that ftp_norm_forward or ftp_ckpt_save left (mean and
+ * rstd stay those of the forward pass).  dx (may be NULL) may be dy or x.  dweight and dbias (device, c floats): both or neither; if
+ * neither, workspace may be NULL.
+ * workspace: device, 16-byte aligned, at least the size ftp_norm_workspace reports (host call); holds the partial sums
+ * of dweight and dbias, and nothing that outlives the call.
+ */
+int ftp_norm_workspace(const ftp_dims* d, size_t* bytes);
+int ftp_norm_backward(const ftp_dims* d, const void* x, long long x_stride, const void* ckpt, const void* dy, long long dy_stride,
+                      const float* weight, const float* mean, const float* rstd, void* dx, long long dx_stride,
+                      float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log probabilities of class labels.  logits z [n, c, p], classes along c; labels: device, n p integers.  For every row
+ *   lse = log sum exp z,  logp = z[label] - lse,  entropy = -sum p log p with p = exp(z - lse) and 0 log 0 = 0,
+ * and the `top` classes of largest logit in descending order, equal ones by lowest class first: top_index [n, top, p] and their
+ * log probabilities top_logp [n, top, p].
+ * A negative label means that the row has none: logp = 0.  A label of c or more gives NaN.  A class that is ruled out has logit
+ * -infinity; it ranks behind every other one.  A row with all classes ruled out has lse = logp = -infinity and entropy 0.  A NaN or +infinity makes all
+ * results of its row NaN except top_index, in which a NaN ranks with the ruled-out classes.  (lse is one fp32: it resolves logits of up
+ * to some thousands; logp, entropy and top_logp are formed from differences to the row's maximum and hold at any magnitude.)
+ * Each output may be NULL, but not all; labels may be NULL if logp is; top_logp and top_index: both or one if top > 0, none if
+ * top = 0.  0 <= top <= FTP_TOP_MAX and top <= c (else FTP_ERR_ARG).  c <= FTP_CLASSES_MAX (else FTP_ERR_TOO_LARGE).
+ */
+#define FTP_TOP_MAX 20
+#define FTP_CLASSES_MAX 260000
+int ftp_logprob(const ftp_dims* d, const void* logits, long long logits_stride, const long long* labels,
+                float* logp, float* lse, float* entropy, int top, float* top_logp, long long* top_index, void* stream);
+
+/*
+ * Gradient of the above: for deltas dlogp and dentropy of each row (device, n p floats, each may be NULL: 0)
+ *   dlogits = dlogp (1[class = label] - p) - dentropy p (log p + entropy),
+ * with the lse and entropy (NULL if dentropy is) that ftp_logprob gave.  Rows without a label take dlogp = 0; a label of c or more
+ * makes its row NaN; a row whose classes are all ruled out gets 0.  dlogits may be logits.
+ */
+int ftp_logprob_backward(const ftp_dims* d, const void* logits, long long logits_stride, const long long* labels,
+                         const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
+                         void* dlogits, long long dlogits_stride, void* stream);
+
+/*
+ * Loss over class labels, beside ftp_loss_mse: L = -(1/M) sum of logp over the M rows that have a label (0 if M = 0), and
+ * dlogits = scale dL/dlogits = (scale / M) (p - 1[class = label]), 0 in rows without a label and in rows whose classes are all ruled out.  `scale` keeps deltas of 16
+ * bits in range (1: none); L is not scaled.  dlogits may be NULL and may be logits; loss_out (device, 1 float) may be NULL; not both.
+ * One pass over the logits.  n p < 2^31 (else FTP_ERR_TOO_LARGE).  workspace: device, 16-byte aligned, at least the size ftp_loss_logprob_workspace reports.
+ */
+int ftp_loss_logprob_workspace(const ftp_dims* d, size_t* bytes);
+int ftp_loss_logprob(const ftp_dims* d, const void* logits, long long logits_stride, const long long* labels, float scale,
+                     void* dlogits, long long dlogits_stride, float* loss_out, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
 const char* ftp_strerror(int code);
 
 #ifdef __cplusplus

@@ -109,6 +109,28 @@ _lib.ftp_plan_check.argtypes = [_vp, _vp, _vp]
 _lib.ftp_plan_check.restype = _i
 _lib.ftp_plan_wait_probe.argtypes = [_vp, _vp, _i, _vp]
 _lib.ftp_plan_wait_probe.restype = _i
+
+
+class ftp_dims(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_int), ("type", ctypes.c_int), ("n", ctypes.c_longlong), ("c", ctypes.c_longlong),
+                ("p", ctypes.c_longlong)]
+
+
+_ll, _f, _dims_p, _sz_p = ctypes.c_longlong, ctypes.c_float, ctypes.POINTER(ftp_dims), ctypes.POINTER(_sz)
+_lib.ftp_ckpt_bytes.argtypes = [_dims_p, _sz_p]
+_lib.ftp_ckpt_save.argtypes = [_dims_p, _vp, _ll, _vp, _vp]
+_lib.ftp_ckpt_load.argtypes = [_dims_p, _vp, _vp, _ll, _vp]
+_lib.ftp_backward_ckpt.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.ftp_norm_workspace.argtypes = [_dims_p, _sz_p]
+_lib.ftp_norm_forward.argtypes = [_dims_p, _vp, _ll, _vp, _vp, _f, _vp, _ll, _vp, _vp, _vp, _vp]
+_lib.ftp_norm_backward.argtypes = [_dims_p, _vp, _ll, _vp, _vp, _ll, _vp, _vp, _vp, _vp, _ll, _vp, _vp, _vp, _sz, _vp]
+_lib.ftp_logprob.argtypes = [_dims_p, _vp, _ll, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp]
+_lib.ftp_logprob_backward.argtypes = [_dims_p, _vp, _ll, _vp, _vp, _vp, _vp, _vp, _vp, _ll, _vp]
+_lib.ftp_loss_logprob_workspace.argtypes = [_dims_p, _sz_p]
+_lib.ftp_loss_logprob.argtypes = [_dims_p, _vp, _ll, _vp, _f, _vp, _ll, _vp, _vp, _sz, _vp]
+for _fn in ("ftp_ckpt_bytes", "ftp_ckpt_save", "ftp_ckpt_load", "ftp_backward_ckpt", "ftp_norm_workspace", "ftp_norm_forward",
+            "ftp_norm_backward", "ftp_logprob", "ftp_logprob_backward", "ftp_loss_logprob_workspace", "ftp_loss_logprob"):
+    getattr(_lib, _fn).restype = _i
 _lib.ftp_strerror.argtypes = [_i]
 _lib.ftp_strerror.restype = ctypes.c_char_p
 
@@ -418,3 +440,223 @@ def ftp_step_host(plan, x_host, target_host, params, lr, loss_host, workspace, d
     ws = _workspace(plan, workspace)
     pp, pdx = _sized((params, "params", plan.param_floats), (dx, "dx", plan.in_floats, True))
     _check(_lib.ftp_step_host(plan._h, px, pt, pp, float(lr), pl, pdx, ws.ptr, _stream(stream)))
+
+
+# ---- operators between and behind the stacks ----------------------------------------------------------------------
+# Arrays are CUDA tensors [n, c] or [n, c, ...] (a 1-D tensor is one row) of float32, bfloat16 or float16, dense within a sample; the first
+# stride is free.  They run on the tensors' own device, on `stream` or that device's current one.
+FTP_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+FTP_TOP_MAX, FTP_CLASSES_MAX = 20, 260000
+
+
+def _shape_of(x, name):
+    """(n, c, p) of a tensor's shape, or of a shape."""
+    shape = tuple(x.shape) if hasattr(x, "shape") else tuple(x)
+    if not shape:
+        raise ValueError(f"{name} must have at least one dimension")
+    if len(shape) == 1:
+        shape = (1,) + shape
+    p = 1
+    for e in shape[2:]:
+        p *= e
+    return shape[0], shape[1], p
+
+
+def _dims(x, name, dtype=None):
+    if dtype is None:
+        dtype = getattr(x, "dtype", torch.float32)
+    if dtype not in FTP_TYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16, not {dtype}")
+    return ftp_dims(ctypes.sizeof(ftp_dims), FTP_TYPES[dtype], *_shape_of(x, name))
+
+
+def _device(x, name):
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    return x.device
+
+
+def _array(t, name, like=None, allow_none=False):
+    """(pointer, elements between samples) of an array: shape and type of `like`, dense within a sample."""
+    if t is None:
+        if allow_none:
+            return None, 0
+        raise ValueError(f"{name} must not be None")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(like.shape)} {like.dtype}")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    n, c, p = _shape_of(t, name)
+    if t.numel() == 0 or t.is_contiguous():
+        return t.data_ptr(), c * p
+    dense, strides = 1, t.stride()
+    for extent, stride in zip(reversed(t.shape[1:]), reversed(strides[1:])):
+        if extent != 1 and stride != dense:
+            raise ValueError(f"{name} must be dense within a sample (strides {strides} for shape {tuple(t.shape)})")
+        dense *= extent
+    if t.dim() == 1 or (n > 1 and strides[0] < c * p):
+        raise ValueError(f"{name}: samples overlap or a row is not dense (strides {strides} for shape {tuple(t.shape)})")
+    return t.data_ptr(), strides[0] if n > 1 else c * p
+
+
+def _plain(t, name, shape, dtype, device, allow_none=False):
+    """Pointer of a contiguous tensor of the given element count, type and device."""
+    if t is None:
+        if allow_none:
+            return None
+        raise ValueError(f"{name} must not be None")
+    count = 1
+    for e in shape:
+        count *= e
+    if t.numel() != count:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {count} {tuple(shape)}")
+    if t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    return t.data_ptr()
+
+
+def _bytes(t, name, need, device):
+    if t is None or not hasattr(t, "data_ptr"):
+        raise ValueError(f"{name} must be a CUDA tensor of at least {need} bytes")
+    have = t.numel() * t.element_size()
+    if have < need:
+        raise ValueError(f"{name} holds {have} bytes, {need} are needed")
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on {device}")
+    return t.data_ptr(), have
+
+
+def _call(fn, device, stream, *args):
+    """The C call with the tensors' device current, on `stream` or that device's current stream."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    s = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, s)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, s)
+    _check(rc)
+
+
+def _size_of(fn, dims):
+    n = _sz()
+    _check(fn(ctypes.byref(dims), ctypes.byref(n)))
+    return n.value
+
+
+def ftp_ckpt_bytes(x):
+    """Bytes of the 8-bit checkpoint of a tensor (or shape)."""
+    return _size_of(_lib.ftp_ckpt_bytes, _dims(x, "x"))
+
+
+def ftp_ckpt_save(x, ckpt, stream=None):
+    """Writes the 8-bit checkpoint of x to ckpt (any contiguous CUDA tensor of ftp_ckpt_bytes(x) bytes)."""
+    d = _dims(x, "x")
+    need, (px, sx) = _size_of(_lib.ftp_ckpt_bytes, d), _array(x, "x")
+    pk = _bytes(ckpt, "ckpt", need, x.device)[0]
+    _call(_lib.ftp_ckpt_save, _device(x, "x"), stream, ctypes.byref(d), px, sx, pk)
+
+
+def ftp_ckpt_load(ckpt, x, stream=None):
+    """Writes the values of a checkpoint to x; shape as when it was saved, any of the three types."""
+    d = _dims(x, "x")
+    need, (px, sx) = _size_of(_lib.ftp_ckpt_bytes, d), _array(x, "x")
+    pk = _bytes(ckpt, "ckpt", need, x.device)[0]
+    _call(_lib.ftp_ckpt_load, _device(x, "x"), stream, ctypes.byref(d), pk, px, sx)
+
+
+def ftp_backward_ckpt(plan, ckpt, x, dy, params, dx, dparams, workspace, stream=None):
+    """ftp_backward with the plan's input taken from a checkpoint: x receives its values, the forward pass runs again."""
+    ws = _workspace(plan, workspace)
+    need = _size_of(_lib.ftp_ckpt_bytes, _dims(plan.shape, "x"))
+    px, pdy, pp, pdx, pg = _sized((x, "x", plan.in_floats), (dy, "dy", plan.out_floats),
+                                  (params, "params", plan.param_floats), (dx, "dx", plan.in_floats, True),
+                                  (dparams, "dparams", plan.param_floats))
+    pk = _bytes(ckpt, "ckpt", need, x.device)[0]
+    _check(_lib.ftp_backward_ckpt(plan._h, pk, px, pdy, pp, pdx, pg, ws.ptr, _stream(stream)))
+
+
+def ftp_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, ckpt=None, stream=None):
+    """y = (x - mean) rstd weight + bias over the channels of each row; ckpt (if given) receives x in 8 bits.  y may be x."""
+    d = _dims(x, "x")
+    (px, sx), (py, sy) = _array(x, "x"), _array(y, "y", x)
+    dev, n, c, p = x.device, d.n, d.c, d.p
+    pw, pb = _plain(weight, "weight", (c,), torch.float32, dev, True), _plain(bias, "bias", (c,), torch.float32, dev, True)
+    pm, pr = _plain(mean, "mean", (n, p), torch.float32, dev, True), _plain(rstd, "rstd", (n, p), torch.float32, dev, True)
+    pk = None if ckpt is None else _bytes(ckpt, "ckpt", _size_of(_lib.ftp_ckpt_bytes, d), dev)[0]
+    _call(_lib.ftp_norm_forward, _device(x, "x"), stream, ctypes.byref(d), px, sx, pw, pb, float(eps), py, sy, pm, pr, pk)
+
+
+def ftp_norm_workspace_bytes(x):
+    """Bytes of the workspace of ftp_norm_backward for a tensor (or shape) x."""
+    return _size_of(_lib.ftp_norm_workspace, _dims(x, "x"))
+
+
+def ftp_norm_backward(x, dy, weight, mean, rstd, dx, dweight, dbias, workspace, ckpt=None, stream=None):
+    """Gradients of ftp_norm_forward, from x or (x None) from its checkpoint; dx, or dweight and dbias (with workspace), may be None."""
+    d = _dims(dy, "dy")
+    if (x is None) == (ckpt is None):
+        raise ValueError("give exactly one of x and ckpt")
+    (pdy, sdy), (px, sx), (pdx, sdx) = _array(dy, "dy"), _array(x, "x", dy, True), _array(dx, "dx", dy, True)
+    dev, n, c, p = dy.device, d.n, d.c, d.p
+    pw = _plain(weight, "weight", (c,), torch.float32, dev, True)
+    pm, pr = _plain(mean, "mean", (n, p), torch.float32, dev), _plain(rstd, "rstd", (n, p), torch.float32, dev)
+    pdw, pdb = _plain(dweight, "dweight", (c,), torch.float32, dev, True), _plain(dbias, "dbias", (c,), torch.float32, dev, True)
+    pk = None if ckpt is None else _bytes(ckpt, "ckpt", _size_of(_lib.ftp_ckpt_bytes, d), dev)[0]
+    pws, nws = (None, 0) if dweight is None else _bytes(workspace, "workspace", _size_of(_lib.ftp_norm_workspace, d), dev)
+    _call(_lib.ftp_norm_backward, _device(dy, "dy"), stream, ctypes.byref(d), px, sx, pk, pdy, sdy, pw, pm, pr, pdx, sdx, pdw, pdb, pws, nws)
+
+
+def ftp_logprob(logits, labels, logp=None, lse=None, entropy=None, top_logp=None, top_index=None, stream=None):
+    """Log probabilities of labels (int64, negative: none), log-sum-exp, entropy and the best classes of each row; outputs that are
+    None are not computed.  top_logp / top_index: [n, k, ...] for the k best, in the place of the classes."""
+    d = _dims(logits, "logits")
+    pz, sz = _array(logits, "logits")
+    dev, n, c, p = logits.device, d.n, d.c, d.p
+    pl = _plain(labels, "labels", (n, p), torch.int64, dev, True)
+    outs = [_plain(t, name, (n, p), torch.float32, dev, True) for t, name in ((logp, "logp"), (lse, "lse"), (entropy, "entropy"))]
+    top = 0
+    for t, name in ((top_logp, "top_logp"), (top_index, "top_index")):
+        if t is None:
+            continue
+        k = _shape_of(t, name)[1]
+        if top and k != top:
+            raise ValueError(f"top_logp and top_index are for {top} and {k} classes")
+        top = k
+        if not 1 <= top <= min(FTP_TOP_MAX, c):
+            raise ValueError(f"{name} is for {top} classes; 1 to {min(FTP_TOP_MAX, c)} can be had")
+    ptl = _plain(top_logp, "top_logp", (n, top, p), torch.float32, dev, True)
+    pti = _plain(top_index, "top_index", (n, top, p), torch.int64, dev, True)
+    _call(_lib.ftp_logprob, _device(logits, "logits"), stream, ctypes.byref(d), pz, sz, pl, *outs, top, ptl, pti)
+
+
+def ftp_logprob_backward(logits, labels, lse, entropy, dlogp, dentropy, dlogits, stream=None):
+    """dlogits from the deltas of logp and entropy (each may be None); dlogits may be logits."""
+    d = _dims(logits, "logits")
+    (pz, sz), (pd, sd) = _array(logits, "logits"), _array(dlogits, "dlogits", logits)
+    dev, rows = logits.device, (d.n, d.p)
+    pl = _plain(labels, "labels", rows, torch.int64, dev, dlogp is None)
+    ps = _plain(lse, "lse", rows, torch.float32, dev)
+    pe = _plain(entropy, "entropy", rows, torch.float32, dev, dentropy is None)
+    pgl, pge = _plain(dlogp, "dlogp", rows, torch.float32, dev, True), _plain(dentropy, "dentropy", rows, torch.float32, dev, True)
+    _call(_lib.ftp_logprob_backward, _device(logits, "logits"), stream, ctypes.byref(d), pz, sz, pl, ps, pe, pgl, pge, pd, sd)
+
+
+def ftp_loss_logprob_workspace_bytes(logits):
+    """Bytes of the workspace of ftp_loss_logprob."""
+    return _size_of(_lib.ftp_loss_logprob_workspace, _dims(logits, "logits"))
+
+
+def ftp_loss_logprob(logits, labels, dlogits, loss_out, workspace, scale=1.0, stream=None):
+    """loss_out = -mean of the log probabilities of the labelled rows, dlogits = scale x its gradient (each may be None, not both;
+    dlogits may be logits)."""
+    d = _dims(logits, "logits")
+    (pz, sz), (pd, sd) = _array(logits, "logits"), _array(dlogits, "dlogits", logits, True)
+    dev = logits.device
+    pl = _plain(labels, "labels", (d.n, d.p), torch.int64, dev)
+    po = _plain(loss_out, "loss_out", (1,), torch.float32, dev, True)
+    pws, nws = _bytes(workspace, "workspace", _size_of(_lib.ftp_loss_logprob_workspace, d), dev)
+    _call(_lib.ftp_loss_logprob, _device(logits, "logits"), stream, ctypes.byref(d), pz, sz, pl, float(scale), pd, sd, po, pws, nws)

@@ -1094,6 +1094,17 @@ int ftp_backward(ftp_plan* plan, const float* x, const float* dy, const float* p
     return backward_impl(plan, x, dy, params, dx, dparams, nullptr, 0.f, workspace, st);
 }
 
+int ftp_backward_ckpt(ftp_plan* plan, const void* ckpt, float* x, const float* dy, const float* params, float* dx, float* dparams,
+                      void* workspace, void* stream)
+{
+    if (!plan || !ckpt || !x || dx == x || !dy || !params || !dparams || !workspace || !aligned256(workspace)) return FTP_ERR_ARG;
+    const MapShape& in = plan->maps.front();
+    const ftp_dims d{(int)sizeof(ftp_dims), FTP_TYPE_F32, plan->N, in.C, (long long)in.H * in.W};
+    int rc = ftp_ckpt_load(&d, ckpt, x, 0, stream);
+    if (rc == FTP_OK) rc = ftp_forward(plan, x, params, nullptr, workspace, stream);
+    return rc == FTP_OK ? ftp_backward(plan, x, dy, params, dx, dparams, workspace, stream) : rc;
+}
+
 static int step_impl(ftp_plan* plan, const float* x, const float* dy, const float* target, const float* params,
                      float* sgd_params, float lr, float* grad_out, float* loss_out, float* dx, void* workspace,
                      void* stream, cudaEvent_t target_ready = nullptr)

@@ -1,0 +1,200 @@
+// What the operators on arrays [n, c, p] share (norm.cu, ckpt.cu, logprob.cu): types, vectors of 16 bytes, sums over a group of
+// threads, the 8-bit checkpoint's arithmetic, host checks.
+//
+// An array is n samples of c channels of p pixels, each sample dense, `stride` elements from one sample to the next; p = 1 is
+// a matrix of n rows.  Values are fp32, bf16 or fp16; every sum and statistic is held in fp32.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "ftp.h"
+#include "launch.cuh"
+
+namespace ftp {
+namespace arr {
+
+constexpr int kSms = 148;                     // multiprocessors of a B200: the unit of the persistent grids
+
+// ---- values -----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+template <class T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+
+template <int BYTES> struct Word;
+template <> struct Word<1> { using type = unsigned char; };
+template <> struct Word<2> { using type = unsigned short; };
+template <> struct Word<4> { using type = unsigned; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
+
+// V values side by side, moved as one word; aligned to its size.
+template <class T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
+
+template <class T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T* p)
+{
+    using W = typename Word<sizeof(T) * V>::type;
+    const W w = *reinterpret_cast<const W*>(p);
+    Pack<T, V> r;
+    __builtin_memcpy(&r, &w, sizeof r);
+    return r;
+}
+template <class T, int V> __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& a)
+{
+    using W = typename Word<sizeof(T) * V>::type;
+    W w;
+    __builtin_memcpy(&w, &a, sizeof w);
+    *reinterpret_cast<W*>(p) = w;
+}
+template <class T, int V> __device__ __forceinline__ Pack<T, V> zero_pack()
+{
+    Pack<T, V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = from_f<T>(0.f);
+    return r;
+}
+
+// Values [e, e + V) of an array of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as 0
+// and is not written.
+template <class T, int V> __device__ __forceinline__ Pack<T, V> load_part(const T* base, long long e, long long lo, long long hi)
+{
+    if (e >= lo && e + V <= hi) return load_pack<T, V>(base + e);
+    Pack<T, V> r = zero_pack<T, V>();
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (e + j >= lo && e + j < hi) r.v[j] = base[e + j];
+    return r;
+}
+template <class T, int V> __device__ __forceinline__ void store_part(T* base, long long e, long long lo, long long hi, const Pack<T, V>& a)
+{
+    if (e >= lo && e + V <= hi) { store_pack<T, V>(base + e, a); return; }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (e + j >= lo && e + j < hi) base[e + j] = a.v[j];
+}
+
+// ---- sums -------------------------------------------------------------------------------------------------------
+// Sum over `width` neighbouring lanes (a power of two); every lane has it.
+__device__ __forceinline__ float lanes_sum(float v, int width)
+{
+    for (int d = width >> 1; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+__device__ __forceinline__ float lanes_max(float v, int width)
+{
+    for (int d = width >> 1; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+
+// ---- the 8-bit checkpoint ---------------------------------------------------------------------------------------
+// Blocks of 32 consecutive values of a row or plane: one byte e stands for the step 2^(e - 127), a signed byte q for the value
+// q * step.  e is the least in [1, 249] with 127 * step >= the largest finite magnitude of the block, so q = round(x / step)
+// is at most 127, both x / step and q * step are exact in fp32, and the value kept is the same bits in every implementation.
+// q = -128 marks an infinity or NaN and reads as NaN.  64 * 2^122 and (fp16) 64 * 2^10 would be infinite: the largest finite
+// values of a type are held to 63 steps.
+constexpr int kBlock = 32;
+constexpr unsigned kFiniteEnd = 0x7f800000u;      // magnitude bits from here on: infinity, NaN
+
+__device__ __forceinline__ unsigned magnitude_bits(float v)
+{
+    const unsigned b = __float_as_uint(v) & 0x7fffffffu;
+    return b < kFiniteEnd ? b : 0u;
+}
+// 127 * 2^k = 1.984375 * 2^(k + 6): the exponent field of the magnitude minus 6, one more if its fraction is above 0x7e0000.
+__device__ __forceinline__ unsigned step_exponent(unsigned largest_bits)
+{
+    const int e = (int)((largest_bits + 0x1ffffu) >> 23) - 6;
+    return e < 1 ? 1u : (unsigned)e;
+}
+__device__ __forceinline__ float step_of(unsigned e) { return __uint_as_float(e << 23); }
+__device__ __forceinline__ float inverse_step(unsigned e) { return __uint_as_float((254u - e) << 23); }
+template <class T> __device__ __forceinline__ float most_steps(unsigned e)
+{
+    return e == 249u || (sizeof(T) == 2 && !__is_same(T, __nv_bfloat16) && e == 137u) ? 63.f : 127.f;
+}
+// The byte q of a value: adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it in the low bits.
+__device__ __forceinline__ unsigned to_steps(float v, float inverse, float most)
+{
+    const float s = fminf(fmaxf(v * inverse, -most), most) + 12582912.f;
+    return (__float_as_uint(v) & 0x7fffffffu) < kFiniteEnd ? __float_as_uint(s) & 0xffu : 0x80u;
+}
+// Values of the four bytes of a word.  A byte plus 128 in the low bits of 2^23 is the float 2^23 + q + 128.
+__device__ __forceinline__ void from_steps(unsigned word, float step, float (&out)[4])
+{
+    const unsigned u = word ^ 0x80808080u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + j)) - 8388736.f) * step;
+    if ((u - 0x01010101u) & ~u & 0x80808080u) {             // a byte of u is 0
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (((word >> (8 * j)) & 0xffu) == 0x80u) out[j] = __uint_as_float(0x7fffffffu);
+    }
+}
+__device__ __forceinline__ float from_step(unsigned char q, float step)
+{
+    return q == 0x80u ? __uint_as_float(0x7fffffffu) : (float)(signed char)q * step;
+}
+
+// Where a checkpoint lies: q bytes of run r (a row or plane of `len` values) at r * pitch, its step bytes at steps + r * blocks.
+struct CkptView {
+    unsigned char* q;
+    unsigned char* steps;
+    long long pitch;
+    int blocks;
+};
+
+// ---- host -------------------------------------------------------------------------------------------------------
+inline int type_size(int type) { return type == FTP_TYPE_F32 ? 4 : 2; }
+
+// FTP_OK with *rows = n * p (0: nothing to do), or an error.  Any count fits 62 bits after this.
+inline int check_dims(const ftp_dims* d, long long* rows)
+{
+    if (!d || d->struct_size != (int)sizeof(ftp_dims)) return FTP_ERR_ARG;
+    if (d->type != FTP_TYPE_F32 && d->type != FTP_TYPE_BF16 && d->type != FTP_TYPE_F16) return FTP_ERR_ARG;
+    if (d->n < 0 || d->c < 1 || d->p < 0) return FTP_ERR_ARG;
+    constexpr long long kMost = 1LL << 30;
+    if (d->n >= kMost || d->c >= kMost || d->p >= kMost) return FTP_ERR_TOO_LARGE;
+    if (d->n > 0 && d->p > 0) {
+        const long long rows_ = d->n * d->p;
+        if (rows_ >= (1LL << 40) || d->c > ((1LL << 46) / rows_)) return FTP_ERR_TOO_LARGE;
+    }
+    *rows = d->n * d->p;
+    return FTP_OK;
+}
+// A sample stride of 0 stands for a dense array; any other must hold a sample.
+inline bool fix_stride(const ftp_dims* d, long long* stride)
+{
+    const long long dense = d->c * d->p;
+    if (*stride == 0) *stride = dense;
+    return *stride >= dense && *stride < (1LL << 46) / (d->n > 0 ? d->n : 1);
+}
+inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Runs that a checkpoint cuts into blocks: the rows of a matrix, or the planes of maps.
+inline long long run_length(const ftp_dims* d) { return d->p == 1 ? d->c : d->p; }
+inline long long run_count(const ftp_dims* d) { return d->p == 1 ? d->n : d->n * d->c; }
+inline CkptView ckpt_view(const ftp_dims* d, const void* ckpt)
+{
+    CkptView v{};
+    v.blocks = (int)((run_length(d) + kBlock - 1) / kBlock);
+    v.pitch = (long long)v.blocks * kBlock;
+    v.q = static_cast<unsigned char*>(const_cast<void*>(ckpt));
+    v.steps = v.q ? v.q + run_count(d) * v.pitch : nullptr;
+    return v;
+}
+
+template <class K> inline bool allow_smem(K kernel, size_t bytes)
+{
+    return bytes <= 48 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+}
+inline int launched() { return cudaGetLastError() == cudaSuccess ? FTP_OK : FTP_ERR_CUDA; }
+
+}  // namespace arr
+}  // namespace ftp

@@ -1,0 +1,160 @@
+// 8-bit checkpoints on their own (ftp_ckpt_bytes, ftp_ckpt_save, ftp_ckpt_load); format and arithmetic in arrays.cuh.
+//
+// Both are bound by memory.  A warp takes segments of a run, all values of a segment in registers; the 32 values of a block lie in
+// 32 / V neighbouring lanes, whose largest magnitude takes log2(32 / V) exchanges.  Where runs are whole blocks and the array is
+// dense, the array is one run: the blocks are the same.
+#include "arrays.cuh"
+
+using namespace ftp;
+using namespace ftp::arr;
+
+namespace {
+
+struct CkptArgs {
+    void* x;
+    CkptView ck;
+    long long runs, len;            // runs of `len` values
+    long long run_stride;           // between runs of a sample
+    long long sample_stride;        // between samples
+    long long per_sample;           // runs of a sample
+};
+
+constexpr int kThreads = 256;
+constexpr int kPer = 4;             // vectors of a lane in a segment
+
+template <class T, int V> __device__ __forceinline__ T* run_at(const CkptArgs& a, long long run)
+{
+    const long long n = run / a.per_sample;
+    return static_cast<T*>(a.x) + n * a.sample_stride + (run - n * a.per_sample) * a.run_stride;
+}
+
+template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads) ckpt_kernel(CkptArgs a, long long segments)
+{
+    previous_launches();
+    constexpr int kSegment = 32 * V * kPer;
+    const int lane = threadIdx.x & 31;
+    const long long warps = (long long)gridDim.x * (kThreads / 32);
+    for (long long task = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); task < a.runs * segments; task += warps) {
+        const long long run = segments == 1 ? task : task / segments;
+        const long long first = (task - run * segments) * kSegment + lane * V;
+        T* x = run_at<T, V>(a, run);
+        unsigned char* q = a.ck.q + run * a.ck.pitch;
+        unsigned char* steps = a.ck.steps + run * a.ck.blocks;
+        if constexpr (SAVE) {
+            Pack<T, V> raw[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const long long e = first + i * 32 * V;
+                raw[i] = e < a.len ? load_part<T, V>(x, e, 0, a.len) : zero_pack<T, V>();
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const long long e = first + i * 32 * V;
+                unsigned big = 0;
+#pragma unroll
+                for (int j = 0; j < V; ++j) big = max(big, magnitude_bits(to_f(raw[i].v[j])));
+#pragma unroll
+                for (int d = kBlock / V / 2; d >= 1; d >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
+                const unsigned ex = step_exponent(big);
+                const float inverse = inverse_step(ex), most = most_steps<T>(ex);
+                Pack<unsigned char, V> b;
+#pragma unroll
+                for (int j = 0; j < V; ++j) b.v[j] = (unsigned char)to_steps(to_f(raw[i].v[j]), inverse, most);
+                if (e < a.ck.pitch) {
+                    store_pack<unsigned char, V>(q + e, b);
+                    if (e % kBlock == 0) steps[e / kBlock] = (unsigned char)ex;
+                }
+            }
+        } else {
+            Pack<unsigned char, V> b[kPer];
+            unsigned char ex[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const long long e = first + i * 32 * V;
+                if (e < a.len) { b[i] = load_pack<unsigned char, V>(q + e); ex[i] = steps[e / kBlock]; }
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const long long e = first + i * 32 * V;
+                if (e >= a.len) continue;
+                Pack<T, V> out;
+                const float step = step_of(ex[i]);
+                if constexpr (V % 4 == 0) {
+#pragma unroll
+                    for (int j = 0; j < V; j += 4) {
+                        unsigned w;
+                        __builtin_memcpy(&w, &b[i].v[j], 4);
+                        float f[4];
+                        from_steps(w, step, f);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) out.v[j + k] = from_f<T>(f[k]);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) out.v[j] = from_f<T>(from_step(b[i].v[j], step));
+                }
+                store_part<T, V>(x, e, 0, a.len, out);
+            }
+        }
+    }
+}
+
+template <class T, int V, bool SAVE> int run(const CkptArgs& a, LaunchStream ls)
+{
+    const long long segment = 32 * V * kPer, segments = (a.ck.pitch + segment - 1) / segment, tasks = a.runs * segments;
+    const long long want = (tasks + kThreads / 32 - 1) / (kThreads / 32), most = 8LL * kSms;
+    launch(ckpt_kernel<T, V, SAVE>, dim3((unsigned)(want < most ? want : most)), dim3(kThreads), 0, ls, a, segments);
+    return launched();
+}
+template <class T, bool SAVE> int pick(const CkptArgs& a, LaunchStream ls)
+{
+    constexpr int V = 16 / sizeof(T);
+    const bool grid = aligned(a.x, 16) && (a.runs == 1 || (a.run_stride % V == 0 && a.sample_stride % V == 0));
+    return grid ? run<T, V, SAVE>(a, ls) : run<T, 1, SAVE>(a, ls);
+}
+
+template <bool SAVE> int ckpt(const ftp_dims* d, const void* x, long long x_stride, const void* ck, void* stream)
+{
+    long long rows = 0;
+    const int rc = check_dims(d, &rows);
+    if (rc != FTP_OK) return rc;
+    if (rows == 0) return FTP_OK;
+    if (!x || !ck || !aligned(x, type_size(d->type)) || !aligned(ck, 16) || !fix_stride(d, &x_stride)) return FTP_ERR_ARG;
+    CkptArgs a{};
+    a.x = const_cast<void*>(x); a.ck = ckpt_view(d, ck);
+    a.len = run_length(d); a.runs = run_count(d); a.run_stride = a.len; a.sample_stride = x_stride; a.per_sample = d->p == 1 ? 1 : d->c;
+    if (a.len % kBlock == 0 && (x_stride == d->c * d->p || d->n == 1) && a.runs * a.ck.blocks < (1LL << 31)) {
+        a.len *= a.runs; a.ck.pitch *= a.runs; a.ck.blocks *= (int)a.runs;
+        a.runs = a.per_sample = 1;
+    }
+    const LaunchStream ls{static_cast<cudaStream_t>(stream), true};
+    if (d->type == FTP_TYPE_F32) return pick<float, SAVE>(a, ls);
+    if (d->type == FTP_TYPE_BF16) return pick<__nv_bfloat16, SAVE>(a, ls);
+    return pick<__half, SAVE>(a, ls);
+}
+
+}  // namespace
+
+extern "C" {
+
+int ftp_ckpt_bytes(const ftp_dims* d, size_t* bytes)
+{
+    long long rows = 0;
+    const int rc = check_dims(d, &rows);
+    if (rc != FTP_OK) return rc;
+    if (!bytes) return FTP_ERR_ARG;
+    *bytes = rows ? (size_t)run_count(d) * (size_t)((run_length(d) + kBlock - 1) / kBlock) * (kBlock + 1) : 0;
+    return FTP_OK;
+}
+
+int ftp_ckpt_save(const ftp_dims* d, const void* x, long long x_stride, void* ck, void* stream)
+{
+    return ckpt<true>(d, x, x_stride, ck, stream);
+}
+
+int ftp_ckpt_load(const ftp_dims* d, const void* ck, void* x, long long x_stride, void* stream)
+{
+    return ckpt<false>(d, x, x_stride, ck, stream);
+}
+
+}  // extern "C"

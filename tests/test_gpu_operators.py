@@ -1,0 +1,509 @@
+"""The channel norm, the 8-bit checkpoints, and the log probabilities of labels with their gradient and loss, against plain
+implementations in 64 bits, at the sizes, layouts and values where they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2409_09083_b200 as ftp
+from _operators import (GUARD, HALF_STEP, TINY, TYPES, U, close, eight_bits, guarded, like, logprob, norm_backward,
+                        norm_forward, rows)
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+# (shape, elements between samples beyond dense, start off a 256-byte boundary): rows of one value to more than a block holds, odd
+# ones, planes that vectors divide and do not, channels from one to more than stay in registers
+SHAPES = [
+    ((1, 1), 0, 0), ((3, 2), 0, 0), ((5, 7), 0, 0), ((33, 32), 0, 0), ((9, 33), 3, 1), ((1, 1024), 0, 0), ((17, 1000), 24, 0),
+    ((6, 1111), 2, 3), ((300, 64), 0, 0), ((4, 4096), 0, 0), ((3, 5001), 0, 0), ((2, 9000), 0, 0), ((2, 20000), 0, 5), ((1, 40000), 8, 0),
+    ((1, 70001), 0, 0), ((700, 257), 1, 0),
+    ((2, 3, 1, 2), 0, 0), ((1, 8, 13, 13), 0, 0), ((3, 32, 13, 13), 0, 0), ((2, 64, 16, 24), 0, 0), ((2, 21, 10, 6), 4, 2), ((1, 512, 7, 7), 0, 0),
+    ((2, 100, 8, 8), 8, 8), ((1, 1030, 5, 4), 0, 0), ((1, 2100, 3, 11), 5, 1), ((40, 5, 1, 3), 0, 0), ((2, 4, 64, 70), 0, 0),
+]
+
+
+def _ids(s):
+    return "x".join(map(str, s[0])) + (f"+{s[1]}" if s[1] else "") + (f"@{s[2]}" if s[2] else "")
+
+
+def _normal(shape, seed, dtype=torch.float32):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+def _run(shape):
+    p = int(np.prod(shape[2:])) if len(shape) > 2 else 1
+    return shape[1] if p == 1 else p
+
+
+def _rows_of(shape):
+    return (shape[0],) + tuple(shape[2:])
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", SHAPES, ids=_ids)
+def test_norm_forward(case, dtype):
+    shape, pad, shift = case
+    x = _normal(shape, 1, dtype) + torch.tensor(0.5, dtype=dtype)
+    w, b = _normal(shape[1:2], 2), _normal(shape[1:2], 3)
+    xd, xg = guarded(x, pad, shift)
+    yd, yg = guarded(torch.zeros_like(x), pad, shift)
+    mean, rstd = (torch.full(_rows_of(shape), GUARD, device="cuda") for _ in range(2))
+    ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
+    ftp.ftp_norm_forward(xd, w.cuda(), b.cuda(), yd, mean, rstd, eps=EPS)
+    y, m, r = norm_forward(x, w, b, EPS)
+    # mean: a sum of c terms in a tree of at most 16 + 5 + 5 levels and one division; 32 half-units of the mean magnitude.  hat: that error
+    # and the ones of variance (the same tree), root and quotient.
+    xr = rows(x)
+    size = xr.abs().mean(1)
+    close(mean, m, 32 * U * size, "mean")
+    err = 64 * U * (1 + (size * r) ** 2)                       # relative error of rstd: the mean's error enters the variance
+    close(rstd, r, err * r, "rstd")
+    hat = (xr.abs() + size[:, None]) * r[:, None]
+    bound = HALF_STEP[dtype] * y.abs() + TINY[dtype] + (64 * U + err[:, None]) * (hat * w.double().abs() + b.double().abs())
+    close(like(rows(yd), shape), like(y, shape), like(bound, shape), "y")
+    xg(), yg()
+    # the same results with the checkpoint on the side, whose bytes are those of the separate call
+    y2, _ = guarded(torch.zeros_like(x), pad, shift)
+    mean2, rstd2 = torch.empty_like(mean), torch.empty_like(rstd)
+    ftp.ftp_norm_forward(xd, w.cuda(), b.cuda(), y2, mean2, rstd2, eps=EPS, ckpt=ckpt)
+    separate = torch.empty_like(ckpt)
+    ftp.ftp_ckpt_save(xd, separate)
+    assert torch.equal(ckpt, separate)
+    close(rows(y2), y, rows(like(bound, shape)), "y beside a checkpoint")
+    # in place, no weight, no statistics
+    y3, _, _ = norm_forward(x, None, None, EPS)
+    ftp.ftp_norm_forward(xd, None, None, xd, eps=EPS)
+    close(rows(xd), y3, HALF_STEP[dtype] * y3.abs() + TINY[dtype] + (64 * U + err[:, None]) * hat, "in place")
+    xg()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("from_ckpt", [False, True])
+@pytest.mark.parametrize("case", SHAPES, ids=_ids)
+def test_norm_backward(case, from_ckpt, dtype):
+    shape, pad, shift = case
+    x = _normal(shape, 4, dtype)
+    dy = _normal(shape, 5, dtype)
+    w = _normal(shape[1:2], 6)
+    xd, xg = guarded(x, pad, shift)
+    dyd, dyg = guarded(dy, pad, shift)
+    dxd, dxg = guarded(torch.zeros_like(x), pad, shift)
+    _, m, r = norm_forward(x, w, None, EPS)
+    mean, rstd = m.float().cuda(), r.float().cuda()
+    dw, db = (torch.full(shape[1:2], GUARD, device="cuda") for _ in range(2))
+    ws = torch.full((ftp.ftp_norm_workspace_bytes(x),), 255, dtype=torch.uint8, device="cuda")      # NaNs, if read before written
+    src = xd
+    x64 = x
+    ckpt = None
+    if from_ckpt:
+        ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
+        ftp.ftp_ckpt_save(xd, ckpt)
+        x64 = torch.from_numpy(eight_bits(x, _run(shape))[0])
+        src = None
+    ftp.ftp_norm_backward(src, dyd, w.cuda(), mean, rstd, dxd, dw, db, ws, ckpt=ckpt)
+    dx, dw64, db64, dx_size, dw_size, db_size = norm_backward(x64, dy, w, mean, rstd)
+    # row sums: trees of at most 8 + 8 + 5 + 5 levels, then five operations: 64 half-units of the terms' magnitude.  Column sums: at most
+    # one thread adds all rows (and the vector's pixels) in turn.
+    close(rows(dxd), dx, HALF_STEP[dtype] * dx.abs() + TINY[dtype] + 64 * U * dx_size, "dx")
+    n = int(np.prod(_rows_of(shape)))
+    close(dw, dw64, (n + 32) * U * dw_size, "dweight")
+    close(db, db64, (n + 32) * U * db_size, "dbias")
+    xg(), dyg(), dxg()
+    # dx in dy's place; dx alone; the sums alone: the same bits
+    dw2, db2 = torch.empty_like(dw), torch.empty_like(db)
+    ftp.ftp_norm_backward(src, dyd, w.cuda(), mean, rstd, None, dw2, db2, ws, ckpt=ckpt)
+    assert torch.equal(dw, dw2) and torch.equal(db, db2)
+    dx2 = torch.empty_like(dxd)
+    if pad == 0 and shift == 0:
+        ftp.ftp_norm_backward(src, dyd, w.cuda(), mean, rstd, dx2, None, None, None, ckpt=ckpt)
+        assert torch.equal(dx2, dxd)
+    ftp.ftp_norm_backward(src, dyd, w.cuda(), mean, rstd, dyd, dw2, db2, ws, ckpt=ckpt)
+    assert torch.equal(dyd, dxd) and torch.equal(dw, dw2)
+    dyg()
+
+
+@pytest.mark.parametrize("shape", [(6, 40), (2, 6, 5, 3)])
+def test_norm_gradients_against_differences(shape):
+    """dx, dweight and dbias against central differences of sum(y t) of the plain forward pass in 64 bits."""
+    x, t, w, b = _normal(shape, 7), _normal(shape, 8), _normal(shape[1:2], 9), _normal(shape[1:2], 10)
+    mean, rstd = (torch.empty(_rows_of(shape), device="cuda") for _ in range(2))
+    y, dx = torch.empty(shape, device="cuda"), torch.empty(shape, device="cuda")
+    dw, db = torch.empty(shape[1], device="cuda"), torch.empty(shape[1], device="cuda")
+    ws = torch.empty(ftp.ftp_norm_workspace_bytes(x), dtype=torch.uint8, device="cuda")
+    ftp.ftp_norm_forward(x.cuda(), w.cuda(), b.cuda(), y, mean, rstd, eps=EPS)
+    ftp.ftp_norm_backward(x.cuda(), t.cuda(), w.cuda(), mean, rstd, dx, dw, db, ws)
+    f = lambda x, w, b: float((norm_forward(x, w, b, EPS)[0] * rows(t)).sum())          # noqa: E731
+    h = 1e-4                                                   # the quotient is off by order h^2 and 2^-53 / h: below 1e-6
+    for name, value, got in (("x", x.double(), dx), ("w", w.double(), dw), ("b", b.double(), db)):
+        flat, args = value.reshape(-1), {"x": x.double(), "w": w.double(), "b": b.double()}
+        for i in range(0, flat.numel(), max(1, flat.numel() // 12)):
+            up, down = flat.clone(), flat.clone()
+            up[i] += h
+            down[i] -= h
+            d = (f(**{**args, name: up.view(value.shape)}) - f(**{**args, name: down.view(value.shape)})) / (2 * h)
+            assert abs(d - float(got.reshape(-1)[i])) <= 2e-5 * max(1.0, float(got.abs().max())), (name, i)
+
+
+@pytest.mark.parametrize("shape", [(5, 300), (2, 12, 9, 4)])
+def test_norm_keeps_a_nan_in_its_row(shape):
+    x = _normal(shape, 11)
+    x.reshape(-1)[7] = float("nan")
+    y = torch.empty(shape, device="cuda")
+    ftp.ftp_norm_forward(x.cuda(), None, None, y, eps=EPS)
+    assert torch.equal(torch.isnan(rows(y)).any(1), torch.isnan(rows(x)).any(1))
+    assert torch.equal(torch.isnan(rows(y)).all(1), torch.isnan(rows(x)).any(1))
+
+
+def test_norm_of_rows_far_from_zero():
+    """(x - mean)^2 is summed, not x^2 - mean^2: values 1000 +- 1 keep their variance."""
+    for shape in ((8, 512), (2, 32, 6, 6)):
+        x = _normal(shape, 12) + 1000
+        mean, rstd = (torch.empty(_rows_of(shape), device="cuda") for _ in range(2))
+        y = torch.empty(shape, device="cuda")
+        ftp.ftp_norm_forward(x.cuda(), None, None, y, mean, rstd, eps=EPS)
+        y64, _, r = norm_forward(x, None, None, EPS)
+        # the mean is off by 32 half-units of 1000, 2e-3, in units of the deviation: squared in the variance
+        close(rstd, r, 1e-5 * r, "rstd")
+        close(rows(y), y64, 32 * U * 1000 * 2 + 1e-4, "y")
+
+
+def _same(a, b):
+    """Equal values, NaN in the same places (an fp16 drawn here may be infinite, and comes back as NaN)."""
+    a, b = a.cpu(), b.cpu()
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(a[~torch.isnan(a)], b[~torch.isnan(b)])
+
+
+# ---- checkpoint -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", SHAPES, ids=_ids)
+def test_ckpt_is_defined_to_the_bit(case, dtype):
+    shape, pad, shift = case
+    x = (_normal(shape, 20) * torch.exp2(6 * _normal(shape, 21))).to(dtype)
+    flat = x.reshape(-1)
+    flat[::13] = 0
+    xd, xg = guarded(x, pad, shift)
+    ckpt = torch.full((ftp.ftp_ckpt_bytes(x) + 64,), 77, dtype=torch.uint8, device="cuda")
+    ftp.ftp_ckpt_save(xd, ckpt)
+    values, q, exponents = eight_bits(x, _run(shape))
+    raw = ckpt.cpu().numpy()
+    assert np.array_equal(raw[:q.size].view(np.int8), q.reshape(-1))
+    assert np.array_equal(raw[q.size:q.size + exponents.size], exponents)
+    assert (raw[q.size + exponents.size:] == 77).all() and q.size + exponents.size == ftp.ftp_ckpt_bytes(x)
+    back, bg = guarded(torch.zeros_like(x), pad, shift)
+    ftp.ftp_ckpt_load(ckpt, back)
+    want = torch.from_numpy(values).to(dtype)
+    assert _same(back, want)
+    xg(), bg()
+    for other in TYPES:
+        o = torch.empty(shape, dtype=other, device="cuda")
+        ftp.ftp_ckpt_load(ckpt, o)
+        assert _same(o, torch.from_numpy(values).float().to(other))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("run", [(4, 96), (3, 45), (2, 3, 7, 9)])
+def test_ckpt_special_values(run, dtype):
+    x = _normal(run, 22).to(dtype)
+    f = x.reshape(-1)
+    top = torch.finfo(dtype).max
+    f[0], f[5], f[11] = float("inf"), float("nan"), -float("inf")
+    f[33], f[34] = top, -top
+    f[35] = torch.finfo(dtype).tiny
+    xd = x.cuda()
+    ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
+    ftp.ftp_ckpt_save(xd, ckpt)
+    back = torch.empty_like(xd)
+    ftp.ftp_ckpt_load(ckpt, back)
+    want = torch.from_numpy(eight_bits(x, _run(run))[0]).to(dtype)
+    assert _same(back, want)
+    assert torch.isfinite(back.cpu()[torch.isfinite(x)]).all()
+
+
+def test_ckpt_of_the_smallest_values():
+    x = torch.tensor([2.0 ** -126, 2.0 ** -127, 2.0 ** -128, 3 * 2.0 ** -127, 2.0 ** -149, 0.0, -(2.0 ** -126)]).reshape(1, 7)
+    ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
+    ftp.ftp_ckpt_save(x.cuda(), ckpt)
+    back = torch.empty((1, 7), device="cuda")
+    ftp.ftp_ckpt_load(ckpt, back)
+    assert torch.equal(back.cpu(), torch.from_numpy(eight_bits(x, 7)[0]).float())
+
+
+# ---- log probabilities ----------------------------------------------------------------------------------------------
+
+CLASSES = [
+    ((1, 1), 0, 0), ((4, 2), 0, 0), ((3, 5), 2, 1), ((65, 32), 0, 0), ((9, 33), 0, 0), ((1, 1000), 0, 0), ((40, 1000), 8, 0), ((7, 1025), 0, 3),
+    ((5, 2049), 0, 0), ((3, 4097), 1, 1), ((2, 20011), 0, 0), ((1, 32000), 0, 0), ((310, 5000), 0, 0), ((1, 131072), 0, 0), ((2, 131071), 0, 0),
+    ((1, 260000), 0, 1),
+    ((1, 2, 1, 3), 0, 0), ((2, 21, 8, 8), 0, 0), ((2, 80, 13, 13), 0, 0), ((1, 300, 9, 12), 8, 0), ((3, 70, 5, 5), 3, 1), ((1, 1500, 3, 4), 0, 0),
+]
+
+
+def _logits(shape, seed, dtype):
+    """Logits with equal values among them, ruled-out classes, rows of one value, of the lowest value, and with nothing left."""
+    z = (3 * _normal(shape, seed)).to(dtype)
+    r = z.movedim(1, -1).reshape(-1, shape[1]).clone()
+    gen = torch.Generator().manual_seed(seed + 1)
+    r[torch.rand(r.shape, generator=gen) < 0.1] = -float("inf")
+    n = r.shape[0]
+    if n >= 4:
+        r[1] = 2.5                                            # all equal
+        r[2] = -float("inf")                                  # nothing left
+        r[3] = torch.finfo(dtype).min                         # masked with the lowest value
+    if n >= 8:
+        r[4, : max(1, shape[1] // 2)] = torch.finfo(dtype).min
+        r[5] = (torch.arange(shape[1]) % 3).to(dtype)         # many equal ones
+    labels = torch.randint(0, shape[1], (n,), generator=gen)
+    labels[::5] = -1
+    if n >= 8:
+        labels[6] = shape[1]                                  # out of range
+    return like(r, shape).contiguous(), labels.reshape(_rows_of(shape))
+
+
+def _lse_bound(z, d):
+    """Half-units: the difference z - m, its product with log2 e (relative to the exponent, weighted with p), the exponential (2 units), a
+    tree of 32 + 16 levels, the logarithm; and for lse the rounding of the sum with m."""
+    return 128 * U
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CLASSES, ids=_ids)
+def test_logprob(case, dtype):
+    shape, pad, shift = case
+    z, labels = _logits(shape, 30, dtype)
+    zd, zg = guarded(z, pad, shift)
+    out = {k: torch.full(_rows_of(shape), GUARD, device="cuda") for k in ("logp", "lse", "entropy")}
+    top = min(shape[1], 20 if shape[0] % 2 else 7)
+    tshape = (shape[0], top) + tuple(shape[2:])
+    tl, ti = torch.full(tshape, GUARD, device="cuda"), torch.full(tshape, -5, dtype=torch.int64, device="cuda")
+    ftp.ftp_logprob(zd, labels.cuda(), top_logp=tl, top_index=ti, **out)
+    want, d, p = logprob(z, labels, top)
+    assert torch.equal(rows(ti).long(), want["top_index"]), "top_index"
+    e = _lse_bound(z, d)
+    fin = torch.where(torch.isfinite(want["lse"]), want["lse"].abs(), torch.zeros(()).double())
+    close(out["lse"], want["lse"], e + U * fin, "lse")
+    lab = torch.where(torch.isfinite(want["logp"]), want["logp"].abs(), torch.zeros(()).double())
+    close(out["logp"], want["logp"], e + 2 * U * lab, "logp")
+    # entropy = log s - (t / s) log 2: each part up to log c and the mean exponent, 32 + 16 levels
+    spread = torch.where(p > 0, p * d.abs(), 0.0).sum(1) + np.log(shape[1]) + 1
+    close(out["entropy"], want["entropy"], e * spread, "entropy")
+    tfin = torch.where(torch.isfinite(want["top_logp"]), want["top_logp"].abs(), torch.zeros(()).double())
+    close(rows(tl), want["top_logp"], e + 2 * U * tfin, "top_logp")
+    zg()
+    # each output alone, and no best classes
+    for k, v in out.items():
+        alone = torch.full_like(v, GUARD)
+        ftp.ftp_logprob(zd, labels.cuda() if k == "logp" else None, **{k: alone})
+        close(alone, v, 0 if len(shape) == 2 else 2 * e * (1 + v.double().abs().nan_to_num(0, 0, 0)), k)
+    one = torch.empty((shape[0], 1) + tuple(shape[2:]), dtype=torch.int64, device="cuda")
+    ftp.ftp_logprob(zd, None, top_index=one)
+    assert torch.equal(one.cpu(), ti[:, :1].cpu())
+
+
+@pytest.mark.parametrize("shape", [(4, 100), (4, 6000), (1, 140000), (1, 12, 2, 2)])
+def test_logprob_of_rows_with_nan_or_infinity(shape):
+    z = 3 * _normal(shape, 31)
+    r = z.movedim(1, -1).reshape(-1, shape[1]).clone()
+    r[0, shape[1] // 2] = float("nan")
+    if r.shape[0] > 1:
+        r[1, 3] = float("inf")
+    z = like(r, shape).contiguous()
+    labels = torch.zeros(_rows_of(shape), dtype=torch.int64)
+    out = {k: torch.empty(_rows_of(shape), device="cuda") for k in ("logp", "lse", "entropy")}
+    ti = torch.empty((shape[0], 5) + tuple(shape[2:]), dtype=torch.int64, device="cuda")
+    ftp.ftp_logprob(z.cuda(), labels.cuda(), top_index=ti, **out)
+    want, _, _ = logprob(z, labels, 5)
+    for k, v in out.items():
+        assert torch.equal(torch.isnan(v.cpu().reshape(-1)), torch.isnan(want[k])), k
+    assert torch.equal(rows(ti).long(), want["top_index"])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CLASSES, ids=_ids)
+def test_logprob_backward(case, dtype):
+    shape, pad, shift = case
+    z, labels = _logits(shape, 32, dtype)
+    r = z.movedim(1, -1).reshape(-1, shape[1])
+    if r.shape[0] >= 4:
+        r[3] = 1.0                                            # (an lse of the lowest value holds no log c: see the header)
+        if r.shape[0] >= 8:
+            r[4] = 0.5
+        z = like(r, shape).contiguous()
+    want, d, p = logprob(z, labels, 1)
+    zd, zg = guarded(z, pad, shift)
+    dz, dg = guarded(torch.zeros_like(z), pad, shift)
+    lse, h = want["lse"].float(), want["entropy"].float()
+    gl, gh = _normal((r.shape[0],), 33), _normal((r.shape[0],), 34)
+    dev = lambda v: v.reshape(_rows_of(shape)).cuda()         # noqa: E731
+    ftp.ftp_logprob_backward(zd, labels.cuda(), dev(lse), dev(h), dev(gl), dev(gh), dz)
+    lab = labels.reshape(-1)
+    wl = torch.where(lab < 0, 0.0, torch.where(lab >= shape[1], torch.nan, gl.double()))[:, None]
+    hit = torch.arange(shape[1])[None] == lab[:, None]
+    zr = rows(z)
+    lp = torch.where(torch.isinf(lse[:, None]), -torch.inf, zr - lse.double()[:, None])
+    pp = torch.exp(lp)
+    want_d = torch.where(hit, wl, 0.0) - pp * wl - gh.double()[:, None] * torch.where(pp > 0, pp * (lp + h.double()[:, None]), 0.0)
+    want_d = torch.where(torch.isinf(lse)[:, None], 0.0, torch.where(torch.isnan(wl), torch.nan, want_d))
+    # z - lse is off by half a unit of the larger of them, the exponent by that and half a unit of itself, the exponential by two units
+    lpf = torch.where(torch.isfinite(lp), lp, 0.0)
+    rel = U * (8 + 2 * lse.double().abs().nan_to_num(0, 0, 0)[:, None] + 3 * lpf.abs())
+    size = hit * wl.abs().nan_to_num() + pp * (wl.abs().nan_to_num() + gh.double().abs()[:, None] * (lpf.abs() + h.double()[:, None] + 1))
+    close(rows(dz), want_d, HALF_STEP[dtype] * want_d.abs().nan_to_num() + TINY[dtype] + 2 * rel * size + 2.0 ** -140, "dlogits")
+    zg(), dg()
+    # one of the deltas alone, in place
+    ftp.ftp_logprob_backward(zd, None, dev(lse), dev(h), None, dev(gh), dz)
+    only = torch.where(torch.isinf(lse)[:, None], 0.0, -gh.double()[:, None] * torch.where(pp > 0, pp * (lp + h.double()[:, None]), 0.0))
+    close(rows(dz), only, HALF_STEP[dtype] * only.abs() + TINY[dtype] + 2 * rel * size + 2.0 ** -140, "dentropy alone")
+    ftp.ftp_logprob_backward(zd, None, dev(lse), dev(h), None, dev(gh), zd)
+    assert torch.equal(zd, dz)
+    zg()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", CLASSES + [((5000, 10), 0, 0), ((3, 4, 60, 61), 0, 0)], ids=_ids)
+def test_loss_logprob(case, dtype):
+    shape, pad, shift = case
+    z, labels = _logits(shape, 35, dtype)
+    n = labels.numel()
+    lab = labels.reshape(-1)
+    lab[lab >= shape[1]] = 0
+    if n >= 4:
+        lab[2] = -1                                           # a row with nothing left would make the loss infinite
+    r = z.movedim(1, -1).reshape(-1, shape[1])
+    for i in range(n):
+        if lab[i] >= 0 and r[i, lab[i]] < -1e30:
+            lab[i] = int(r[i].argmax())                       # nor a label that is ruled out
+    zd, zg = guarded(z, pad, shift)
+    dz, dg = guarded(torch.zeros_like(z), pad, shift)
+    loss = torch.full((1,), GUARD, device="cuda")
+    ws = torch.full((ftp.ftp_loss_logprob_workspace_bytes(z),), 255, dtype=torch.uint8, device="cuda")
+    scale = 1024.0
+    ftp.ftp_loss_logprob(zd, labels.cuda(), dz, loss, ws, scale=scale)
+    want, d, p = logprob(z, labels, 1)
+    known = lab >= 0
+    m = max(1, int(known.sum()))
+    hit = torch.arange(shape[1])[None] == lab[:, None]
+    want_d = torch.where(known[:, None], (p - hit.double()) * (scale / m), 0.0)
+    df = torch.where(torch.isfinite(d), d, 0.0)
+    bound = HALF_STEP[dtype] * want_d.abs() + TINY[dtype] + U * (64 + 4 * df.abs()) * (p + hit) * known[:, None] * (scale / m) + 2.0 ** -140
+    close(rows(dz), want_d, bound, "dlogits")
+    terms = want["logp"][known].abs().sum() / m
+    close(loss[0], -want["logp"][known].sum() / m, (128 + 16 + n) * U * (terms + 1), "loss")
+    zg(), dg()
+    # loss alone, delta alone, delta in the logits' place: the same bits
+    loss2, dz2 = torch.empty_like(loss), torch.empty_like(dz)
+    ftp.ftp_loss_logprob(zd, labels.cuda(), None, loss2, ws, scale=scale)
+    ftp.ftp_loss_logprob(zd, labels.cuda(), zd, None, ws, scale=scale)
+    assert torch.equal(loss, loss2) and torch.equal(zd, dz)
+    zg()
+
+
+def test_loss_without_a_labelled_row_and_with_ruled_out_ones():
+    for shape in ((6, 50), (2, 5, 3, 3)):
+        z = _normal(shape, 36).cuda()
+        none = torch.full(_rows_of(shape), -1, dtype=torch.int64, device="cuda")
+        ws = torch.empty(ftp.ftp_loss_logprob_workspace_bytes(z), dtype=torch.uint8, device="cuda")
+        loss, dz = torch.full((1,), GUARD, device="cuda"), torch.full(shape, GUARD, device="cuda")
+        ftp.ftp_loss_logprob(z, none, dz, loss, ws)
+        assert loss.item() == 0.0 and not dz.any()
+        z.movedim(1, -1)[0].reshape(-1, shape[1])[:] = -float("inf")
+        if len(shape) == 4:
+            z[0] = -float("inf")
+        ftp.ftp_loss_logprob(z, none + 1, dz, loss, ws)
+        assert loss.item() == float("inf") and torch.isfinite(dz).all() and not dz[0].any()
+        ftp.ftp_loss_logprob(z, none + 1 + shape[1], dz, loss, ws)
+        assert torch.isnan(loss).all() and torch.isnan(dz).all()
+
+
+@pytest.mark.parametrize("shape", [(5, 9), (1, 4, 3, 2)])
+def test_loss_gradient_against_differences(shape):
+    z = _normal(shape, 37)
+    labels = torch.randint(0, shape[1], _rows_of(shape), generator=torch.Generator().manual_seed(1))
+    dz, loss = torch.empty(shape, device="cuda"), torch.empty(1, device="cuda")
+    ws = torch.empty(ftp.ftp_loss_logprob_workspace_bytes(z), dtype=torch.uint8, device="cuda")
+    ftp.ftp_loss_logprob(z.cuda(), labels.cuda(), dz, loss, ws)
+    f = lambda v: -float(logprob(v.view(shape), labels, 1)[0]["logp"].mean())       # noqa: E731
+    flat, h = z.double().reshape(-1), 1e-4
+    for i in range(flat.numel()):
+        up, down = flat.clone(), flat.clone()
+        up[i] += h
+        down[i] -= h
+        assert abs((f(up) - f(down)) / (2 * h) - float(dz.reshape(-1)[i])) <= 1e-6
+
+
+# ---- streams, graphs, order -----------------------------------------------------------------------------------------
+
+def _everything(x, dy, w, labels, out):
+    ftp.ftp_norm_forward(x, w, w, out["y"], out["mean"], out["rstd"], ckpt=out["ckpt"])
+    ftp.ftp_loss_logprob(out["y"], labels, out["dz"], out["loss"], out["lws"])
+    ftp.ftp_logprob(out["y"], labels, out["logp"], out["lse"], out["entropy"], out["tl"], out["ti"])
+    ftp.ftp_logprob_backward(out["y"], labels, out["lse"], out["entropy"], dy[:, 0], out["logp"], out["dz2"])
+    ftp.ftp_norm_backward(None, out["dz"], w, out["mean"], out["rstd"], out["dx"], out["dw"], out["db"], out["nws"], ckpt=out["ckpt"])
+    ftp.ftp_ckpt_load(out["ckpt"], out["back"])
+
+
+def _buffers(x, labels):
+    rs = labels.shape
+    out = {k: torch.empty_like(x) for k in ("y", "dz", "dz2", "dx", "back")}
+    out |= {k: torch.empty(rs, device="cuda") for k in ("mean", "rstd", "logp", "lse", "entropy")}
+    out |= {"tl": torch.empty((x.shape[0], 4) + x.shape[2:], device="cuda"),
+            "ti": torch.empty((x.shape[0], 4) + x.shape[2:], device="cuda", dtype=torch.int64),
+            "loss": torch.empty(1, device="cuda"), "dw": torch.empty(x.shape[1], device="cuda"), "db": torch.empty(x.shape[1], device="cuda"),
+            "ckpt": torch.empty(ftp.ftp_ckpt_bytes(x), device="cuda", dtype=torch.uint8),
+            "nws": torch.empty(ftp.ftp_norm_workspace_bytes(x), device="cuda", dtype=torch.uint8),
+            "lws": torch.empty(ftp.ftp_loss_logprob_workspace_bytes(x), device="cuda", dtype=torch.uint8)}
+    return out
+
+
+_RESULTS = ("y", "dz", "dz2", "dx", "back", "mean", "rstd", "logp", "lse", "entropy", "tl", "ti", "loss", "dw", "db", "ckpt")
+
+
+@pytest.mark.parametrize("shape", [(600, 1003), (3, 5000), (1, 130000), (3, 40, 19, 19)])
+def test_graph_side_stream_and_repeat_give_the_same_bits(shape):
+    labels = torch.randint(-1, shape[1], _rows_of(shape), generator=torch.Generator().manual_seed(2)).cuda()
+    w = _normal(shape[1:2], 40).cuda()
+    x, dy = _normal(shape, 41).cuda(), _normal(shape, 42).cuda()
+    dy0 = dy.select(1, 0).contiguous()
+    pack = dy0.unsqueeze(1)                                   # dy[:, 0] of _everything: one delta for each row
+    first = _buffers(x, labels)
+    _everything(x, pack, w, labels, first)
+    again = _buffers(x, labels)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _everything(x, pack, w, labels, again)
+    torch.cuda.synchronize()
+    held = _buffers(x, labels)
+    xs = torch.zeros_like(x)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _everything(xs, pack, w, labels, held)
+    xs.copy_(x)
+    g.replay()
+    torch.cuda.synchronize()
+    for k in _RESULTS:
+        assert torch.equal(first[k], again[k]), k
+        assert torch.equal(first[k], held[k]), k
+
+
+def test_empty_arrays():
+    w = torch.full((6,), GUARD, device="cuda")
+    for shape in ((0, 6), (2, 6, 0, 3)):
+        x = torch.empty(shape, device="cuda")
+        labels = torch.empty(_rows_of(shape), dtype=torch.int64, device="cuda")
+        stat = torch.empty(_rows_of(shape), device="cuda")
+        ws = torch.empty(ftp.ftp_norm_workspace_bytes(x), dtype=torch.uint8, device="cuda")
+        assert ftp.ftp_ckpt_bytes(x) == 0
+        ftp.ftp_norm_forward(x, w, None, x, stat, stat)
+        dw, db = w.clone(), w.clone()
+        ftp.ftp_norm_backward(x, x, w, stat, stat, x, dw, db, ws)
+        assert not dw.any() and not db.any()
+        ftp.ftp_norm_backward(x, x, w, stat, stat, x, None, None, None)
+        ftp.ftp_loss_logprob(x, labels, x, None, torch.empty(ftp.ftp_loss_logprob_workspace_bytes(x), dtype=torch.uint8, device="cuda"))
+        ftp.ftp_logprob(x, labels, stat)
+        ftp.ftp_logprob_backward(x, labels, stat, None, stat, None, x)
+        loss = torch.full((1,), GUARD, device="cuda")
+        ftp.ftp_loss_logprob(x, labels, x, loss, torch.empty(ftp.ftp_loss_logprob_workspace_bytes(x), dtype=torch.uint8, device="cuda"))
+        assert loss.item() == 0.0
