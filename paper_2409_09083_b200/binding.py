@@ -5,6 +5,7 @@ built the import fails; there is no CPU fallback.  Tensors are torch CUDA
 tensors (fp32, contiguous); torch is used for device memory and streams only.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -449,67 +450,74 @@ FTP_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 FTP_TOP_MAX, FTP_CLASSES_MAX = 20, 260000
 
 
-def _shape_of(x, name):
-    """(n, c, p) of a tensor's shape, or of a shape."""
-    shape = tuple(x.shape) if hasattr(x, "shape") else tuple(x)
-    if not shape:
+class _Dims:
+    """What the calls need to know of a shape and type: the C struct, counts, and the sizes the library reports (asked for once)."""
+
+    def __init__(self, shape, dtype):
+        self.n, self.c = (1, shape[0]) if len(shape) == 1 else shape[:2]
+        self.p = 1
+        for e in shape[2:]:
+            self.p *= e
+        self.rows = self.n * self.p
+        self.struct = ftp_dims(ctypes.sizeof(ftp_dims), FTP_TYPES[dtype], self.n, self.c, self.p)
+        self.ref = ctypes.byref(self.struct)
+        self._sizes = {}
+
+    def size(self, entry):
+        if entry not in self._sizes:
+            n = _sz()
+            _check(getattr(_lib, entry)(self.ref, ctypes.byref(n)))
+            self._sizes[entry] = n.value
+        return self._sizes[entry]
+
+
+_dims_of = functools.lru_cache(maxsize=1024)(_Dims)
+
+
+def _dims(x, name):
+    """_Dims of a tensor, or of a shape (as float32)."""
+    if hasattr(x, "dtype"):
+        if x.dtype not in FTP_TYPES:
+            raise ValueError(f"{name} must be float32, bfloat16 or float16, not {x.dtype}")
+        if x.dim() == 0:
+            raise ValueError(f"{name} must have at least one dimension")
+        return _dims_of(x.shape, x.dtype)
+    if not len(x):
         raise ValueError(f"{name} must have at least one dimension")
-    if len(shape) == 1:
-        shape = (1,) + shape
-    p = 1
-    for e in shape[2:]:
-        p *= e
-    return shape[0], shape[1], p
-
-
-def _dims(x, name, dtype=None):
-    if dtype is None:
-        dtype = getattr(x, "dtype", torch.float32)
-    if dtype not in FTP_TYPES:
-        raise ValueError(f"{name} must be float32, bfloat16 or float16, not {dtype}")
-    return ftp_dims(ctypes.sizeof(ftp_dims), FTP_TYPES[dtype], *_shape_of(x, name))
-
-
-def _device(x, name):
-    if not x.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    return x.device
+    return _dims_of(tuple(x), torch.float32)
 
 
 def _array(t, name, like=None, allow_none=False):
-    """(pointer, elements between samples) of an array: shape and type of `like`, dense within a sample."""
+    """(pointer, elements between samples; 0: dense) of an array: shape, type and device of `like`, dense within a sample."""
     if t is None:
         if allow_none:
             return None, 0
         raise ValueError(f"{name} must not be None")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(like.shape)} {like.dtype}")
-    if like is not None and t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
-    n, c, p = _shape_of(t, name)
-    if t.numel() == 0 or t.is_contiguous():
-        return t.data_ptr(), c * p
+    if like is not None and t is not like:
+        if t.shape != like.shape or t.dtype != like.dtype:
+            raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, expected {tuple(like.shape)} {like.dtype}")
+        if t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t.is_contiguous() or t.numel() == 0:
+        return t.data_ptr(), 0
     dense, strides = 1, t.stride()
     for extent, stride in zip(reversed(t.shape[1:]), reversed(strides[1:])):
         if extent != 1 and stride != dense:
             raise ValueError(f"{name} must be dense within a sample (strides {strides} for shape {tuple(t.shape)})")
         dense *= extent
-    if t.dim() == 1 or (n > 1 and strides[0] < c * p):
+    if t.dim() == 1 or (t.shape[0] > 1 and strides[0] < dense):
         raise ValueError(f"{name}: samples overlap or a row is not dense (strides {strides} for shape {tuple(t.shape)})")
-    return t.data_ptr(), strides[0] if n > 1 else c * p
+    return t.data_ptr(), strides[0] if t.shape[0] > 1 else 0
 
 
-def _plain(t, name, shape, dtype, device, allow_none=False):
+def _plain(t, name, count, dtype, device, allow_none=False):
     """Pointer of a contiguous tensor of the given element count, type and device."""
     if t is None:
         if allow_none:
             return None
         raise ValueError(f"{name} must not be None")
-    count = 1
-    for e in shape:
-        count *= e
     if t.numel() != count:
-        raise ValueError(f"{name} has {t.numel()} elements, expected {count} {tuple(shape)}")
+        raise ValueError(f"{name} has {t.numel()} elements, expected {count}")
     if t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor")
     if t.device != device:
@@ -518,6 +526,7 @@ def _plain(t, name, shape, dtype, device, allow_none=False):
 
 
 def _bytes(t, name, need, device):
+    """(pointer, size) of a buffer of at least `need` bytes."""
     if t is None or not hasattr(t, "data_ptr"):
         raise ValueError(f"{name} must be a CUDA tensor of at least {need} bytes")
     have = t.numel() * t.element_size()
@@ -528,135 +537,127 @@ def _bytes(t, name, need, device):
     return t.data_ptr(), have
 
 
-def _call(fn, device, stream, *args):
-    """The C call with the tensors' device current, on `stream` or that device's current stream."""
+def _call(fn, x, name, stream, *args):
+    """The C call with the device of x current, on `stream` or that device's current stream."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    index = x.get_device()
     if stream is None:
-        stream = torch.cuda.current_stream(device)
-    s = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, s)
+        # (the handle itself: building a torch.cuda.Stream object takes 2 us)
+        stream = torch._C._cuda_getCurrentRawStream(index)
+    elif hasattr(stream, "cuda_stream"):
+        stream = stream.cuda_stream
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, s)
-    _check(rc)
-
-
-def _size_of(fn, dims):
-    n = _sz()
-    _check(fn(ctypes.byref(dims), ctypes.byref(n)))
-    return n.value
+        stream = int(stream)
+    if index == torch._C._cuda_getDevice():
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, stream)
+    if rc != 0:
+        raise FtpError(rc)
 
 
 def ftp_ckpt_bytes(x):
     """Bytes of the 8-bit checkpoint of a tensor (or shape)."""
-    return _size_of(_lib.ftp_ckpt_bytes, _dims(x, "x"))
+    return _dims(x, "x").size("ftp_ckpt_bytes")
 
 
 def ftp_ckpt_save(x, ckpt, stream=None):
     """Writes the 8-bit checkpoint of x to ckpt (any contiguous CUDA tensor of ftp_ckpt_bytes(x) bytes)."""
-    d = _dims(x, "x")
-    need, (px, sx) = _size_of(_lib.ftp_ckpt_bytes, d), _array(x, "x")
-    pk = _bytes(ckpt, "ckpt", need, x.device)[0]
-    _call(_lib.ftp_ckpt_save, _device(x, "x"), stream, ctypes.byref(d), px, sx, pk)
+    d, (px, sx) = _dims(x, "x"), _array(x, "x")
+    pk = _bytes(ckpt, "ckpt", d.size("ftp_ckpt_bytes"), x.device)[0]
+    _call(_lib.ftp_ckpt_save, x, "x", stream, d.ref, px, sx, pk)
 
 
 def ftp_ckpt_load(ckpt, x, stream=None):
     """Writes the values of a checkpoint to x; shape as when it was saved, any of the three types."""
-    d = _dims(x, "x")
-    need, (px, sx) = _size_of(_lib.ftp_ckpt_bytes, d), _array(x, "x")
-    pk = _bytes(ckpt, "ckpt", need, x.device)[0]
-    _call(_lib.ftp_ckpt_load, _device(x, "x"), stream, ctypes.byref(d), pk, px, sx)
+    d, (px, sx) = _dims(x, "x"), _array(x, "x")
+    pk = _bytes(ckpt, "ckpt", d.size("ftp_ckpt_bytes"), x.device)[0]
+    _call(_lib.ftp_ckpt_load, x, "x", stream, d.ref, pk, px, sx)
 
 
 def ftp_backward_ckpt(plan, ckpt, x, dy, params, dx, dparams, workspace, stream=None):
     """ftp_backward with the plan's input taken from a checkpoint: x receives its values, the forward pass runs again."""
     ws = _workspace(plan, workspace)
-    need = _size_of(_lib.ftp_ckpt_bytes, _dims(plan.shape, "x"))
     px, pdy, pp, pdx, pg = _sized((x, "x", plan.in_floats), (dy, "dy", plan.out_floats),
                                   (params, "params", plan.param_floats), (dx, "dx", plan.in_floats, True),
                                   (dparams, "dparams", plan.param_floats))
-    pk = _bytes(ckpt, "ckpt", need, x.device)[0]
+    pk = _bytes(ckpt, "ckpt", ftp_ckpt_bytes(plan.shape), x.device)[0]
     _check(_lib.ftp_backward_ckpt(plan._h, pk, px, pdy, pp, pdx, pg, ws.ptr, _stream(stream)))
 
 
 def ftp_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, ckpt=None, stream=None):
     """y = (x - mean) rstd weight + bias over the channels of each row; ckpt (if given) receives x in 8 bits.  y may be x."""
-    d = _dims(x, "x")
+    d, dev, f32 = _dims(x, "x"), x.device, torch.float32
     (px, sx), (py, sy) = _array(x, "x"), _array(y, "y", x)
-    dev, n, c, p = x.device, d.n, d.c, d.p
-    pw, pb = _plain(weight, "weight", (c,), torch.float32, dev, True), _plain(bias, "bias", (c,), torch.float32, dev, True)
-    pm, pr = _plain(mean, "mean", (n, p), torch.float32, dev, True), _plain(rstd, "rstd", (n, p), torch.float32, dev, True)
-    pk = None if ckpt is None else _bytes(ckpt, "ckpt", _size_of(_lib.ftp_ckpt_bytes, d), dev)[0]
-    _call(_lib.ftp_norm_forward, _device(x, "x"), stream, ctypes.byref(d), px, sx, pw, pb, float(eps), py, sy, pm, pr, pk)
+    pw, pb = _plain(weight, "weight", d.c, f32, dev, True), _plain(bias, "bias", d.c, f32, dev, True)
+    pm, pr = _plain(mean, "mean", d.rows, f32, dev, True), _plain(rstd, "rstd", d.rows, f32, dev, True)
+    pk = None if ckpt is None else _bytes(ckpt, "ckpt", d.size("ftp_ckpt_bytes"), dev)[0]
+    _call(_lib.ftp_norm_forward, x, "x", stream, d.ref, px, sx, pw, pb, float(eps), py, sy, pm, pr, pk)
 
 
 def ftp_norm_workspace_bytes(x):
     """Bytes of the workspace of ftp_norm_backward for a tensor (or shape) x."""
-    return _size_of(_lib.ftp_norm_workspace, _dims(x, "x"))
+    return _dims(x, "x").size("ftp_norm_workspace")
 
 
 def ftp_norm_backward(x, dy, weight, mean, rstd, dx, dweight, dbias, workspace, ckpt=None, stream=None):
     """Gradients of ftp_norm_forward, from x or (x None) from its checkpoint; dx, or dweight and dbias (with workspace), may be None."""
-    d = _dims(dy, "dy")
+    d, dev, f32 = _dims(dy, "dy"), dy.device, torch.float32
     if (x is None) == (ckpt is None):
         raise ValueError("give exactly one of x and ckpt")
     (pdy, sdy), (px, sx), (pdx, sdx) = _array(dy, "dy"), _array(x, "x", dy, True), _array(dx, "dx", dy, True)
-    dev, n, c, p = dy.device, d.n, d.c, d.p
-    pw = _plain(weight, "weight", (c,), torch.float32, dev, True)
-    pm, pr = _plain(mean, "mean", (n, p), torch.float32, dev), _plain(rstd, "rstd", (n, p), torch.float32, dev)
-    pdw, pdb = _plain(dweight, "dweight", (c,), torch.float32, dev, True), _plain(dbias, "dbias", (c,), torch.float32, dev, True)
-    pk = None if ckpt is None else _bytes(ckpt, "ckpt", _size_of(_lib.ftp_ckpt_bytes, d), dev)[0]
-    pws, nws = (None, 0) if dweight is None else _bytes(workspace, "workspace", _size_of(_lib.ftp_norm_workspace, d), dev)
-    _call(_lib.ftp_norm_backward, _device(dy, "dy"), stream, ctypes.byref(d), px, sx, pk, pdy, sdy, pw, pm, pr, pdx, sdx, pdw, pdb, pws, nws)
+    pw = _plain(weight, "weight", d.c, f32, dev, True)
+    pm, pr = _plain(mean, "mean", d.rows, f32, dev), _plain(rstd, "rstd", d.rows, f32, dev)
+    pdw, pdb = _plain(dweight, "dweight", d.c, f32, dev, True), _plain(dbias, "dbias", d.c, f32, dev, True)
+    pk = None if ckpt is None else _bytes(ckpt, "ckpt", d.size("ftp_ckpt_bytes"), dev)[0]
+    pws, nws = (None, 0) if dweight is None else _bytes(workspace, "workspace", d.size("ftp_norm_workspace"), dev)
+    _call(_lib.ftp_norm_backward, dy, "dy", stream, d.ref, px, sx, pk, pdy, sdy, pw, pm, pr, pdx, sdx, pdw, pdb, pws, nws)
 
 
 def ftp_logprob(logits, labels, logp=None, lse=None, entropy=None, top_logp=None, top_index=None, stream=None):
     """Log probabilities of labels (int64, negative: none), log-sum-exp, entropy and the best classes of each row; outputs that are
     None are not computed.  top_logp / top_index: [n, k, ...] for the k best, in the place of the classes."""
-    d = _dims(logits, "logits")
-    pz, sz = _array(logits, "logits")
-    dev, n, c, p = logits.device, d.n, d.c, d.p
-    pl = _plain(labels, "labels", (n, p), torch.int64, dev, True)
-    outs = [_plain(t, name, (n, p), torch.float32, dev, True) for t, name in ((logp, "logp"), (lse, "lse"), (entropy, "entropy"))]
+    d, (pz, sz), dev, f32 = _dims(logits, "logits"), _array(logits, "logits"), logits.device, torch.float32
+    pl = _plain(labels, "labels", d.rows, torch.int64, dev, True)
+    po, ps, pe = (_plain(logp, "logp", d.rows, f32, dev, True), _plain(lse, "lse", d.rows, f32, dev, True),
+                  _plain(entropy, "entropy", d.rows, f32, dev, True))
     top = 0
     for t, name in ((top_logp, "top_logp"), (top_index, "top_index")):
         if t is None:
             continue
-        k = _shape_of(t, name)[1]
+        k = t.shape[min(1, t.dim() - 1)] if t.dim() else 0
         if top and k != top:
             raise ValueError(f"top_logp and top_index are for {top} and {k} classes")
         top = k
-        if not 1 <= top <= min(FTP_TOP_MAX, c):
-            raise ValueError(f"{name} is for {top} classes; 1 to {min(FTP_TOP_MAX, c)} can be had")
-    ptl = _plain(top_logp, "top_logp", (n, top, p), torch.float32, dev, True)
-    pti = _plain(top_index, "top_index", (n, top, p), torch.int64, dev, True)
-    _call(_lib.ftp_logprob, _device(logits, "logits"), stream, ctypes.byref(d), pz, sz, pl, *outs, top, ptl, pti)
+        if not 1 <= top <= min(FTP_TOP_MAX, d.c):
+            raise ValueError(f"{name} is for {top} classes; 1 to {min(FTP_TOP_MAX, d.c)} can be had")
+    ptl, pti = _plain(top_logp, "top_logp", d.rows * top, f32, dev, True), _plain(top_index, "top_index", d.rows * top, torch.int64, dev, True)
+    _call(_lib.ftp_logprob, logits, "logits", stream, d.ref, pz, sz, pl, po, ps, pe, top, ptl, pti)
 
 
 def ftp_logprob_backward(logits, labels, lse, entropy, dlogp, dentropy, dlogits, stream=None):
     """dlogits from the deltas of logp and entropy (each may be None); dlogits may be logits."""
-    d = _dims(logits, "logits")
+    d, dev, f32 = _dims(logits, "logits"), logits.device, torch.float32
     (pz, sz), (pd, sd) = _array(logits, "logits"), _array(dlogits, "dlogits", logits)
-    dev, rows = logits.device, (d.n, d.p)
-    pl = _plain(labels, "labels", rows, torch.int64, dev, dlogp is None)
-    ps = _plain(lse, "lse", rows, torch.float32, dev)
-    pe = _plain(entropy, "entropy", rows, torch.float32, dev, dentropy is None)
-    pgl, pge = _plain(dlogp, "dlogp", rows, torch.float32, dev, True), _plain(dentropy, "dentropy", rows, torch.float32, dev, True)
-    _call(_lib.ftp_logprob_backward, _device(logits, "logits"), stream, ctypes.byref(d), pz, sz, pl, ps, pe, pgl, pge, pd, sd)
+    pl = _plain(labels, "labels", d.rows, torch.int64, dev, dlogp is None)
+    ps, pe = _plain(lse, "lse", d.rows, f32, dev), _plain(entropy, "entropy", d.rows, f32, dev, dentropy is None)
+    pgl, pge = _plain(dlogp, "dlogp", d.rows, f32, dev, True), _plain(dentropy, "dentropy", d.rows, f32, dev, True)
+    _call(_lib.ftp_logprob_backward, logits, "logits", stream, d.ref, pz, sz, pl, ps, pe, pgl, pge, pd, sd)
 
 
 def ftp_loss_logprob_workspace_bytes(logits):
     """Bytes of the workspace of ftp_loss_logprob."""
-    return _size_of(_lib.ftp_loss_logprob_workspace, _dims(logits, "logits"))
+    return _dims(logits, "logits").size("ftp_loss_logprob_workspace")
 
 
 def ftp_loss_logprob(logits, labels, dlogits, loss_out, workspace, scale=1.0, stream=None):
     """loss_out = -mean of the log probabilities of the labelled rows, dlogits = scale x its gradient (each may be None, not both;
     dlogits may be logits)."""
-    d = _dims(logits, "logits")
+    d, dev = _dims(logits, "logits"), logits.device
     (pz, sz), (pd, sd) = _array(logits, "logits"), _array(dlogits, "dlogits", logits, True)
-    dev = logits.device
-    pl = _plain(labels, "labels", (d.n, d.p), torch.int64, dev)
-    po = _plain(loss_out, "loss_out", (1,), torch.float32, dev, True)
-    pws, nws = _bytes(workspace, "workspace", _size_of(_lib.ftp_loss_logprob_workspace, d), dev)
-    _call(_lib.ftp_loss_logprob, _device(logits, "logits"), stream, ctypes.byref(d), pz, sz, pl, float(scale), pd, sd, po, pws, nws)
+    pl = _plain(labels, "labels", d.rows, torch.int64, dev)
+    po = _plain(loss_out, "loss_out", 1, torch.float32, dev, True)
+    pws, nws = _bytes(workspace, "workspace", d.size("ftp_loss_logprob_workspace"), dev)
+    _call(_lib.ftp_loss_logprob, logits, "logits", stream, d.ref, pz, sz, pl, float(scale), pd, sd, po, pws, nws)

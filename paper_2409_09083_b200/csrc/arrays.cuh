@@ -80,18 +80,159 @@ template <class T, int V> __device__ __forceinline__ void store_part(T* base, lo
         if (e + j >= lo && e + j < hi) base[e + j] = a.v[j];
 }
 
+// V values as fp32, in pairs where V is even: the packed fp32 instructions of sm_100 do two values in one issue slot, and all of
+// the kernels here are closer to the issue rate than to anything else but memory.
+__device__ __forceinline__ unsigned long long pair(float a, float b)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(unsigned long long p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+
+template <int V> struct Vals { float v[V]; };
+
+template <int V> __device__ __forceinline__ Vals<V> all(float s)
+{
+    Vals<V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = s;
+    return r;
+}
+template <int V> __device__ __forceinline__ Vals<V> fma(const Vals<V>& a, const Vals<V>& b, const Vals<V>& c)
+{
+    Vals<V> r;
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            unsigned long long d;
+            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(pair(a.v[j], a.v[j + 1])), "l"(pair(b.v[j], b.v[j + 1])), "l"(pair(c.v[j], c.v[j + 1])));
+            split(d, r.v[j], r.v[j + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = fmaf(a.v[j], b.v[j], c.v[j]);
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ Vals<V> add(const Vals<V>& a, const Vals<V>& b)
+{
+    Vals<V> r;
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            unsigned long long d;
+            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair(a.v[j], a.v[j + 1])), "l"(pair(b.v[j], b.v[j + 1])));
+            split(d, r.v[j], r.v[j + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = a.v[j] + b.v[j];
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ Vals<V> mul(const Vals<V>& a, const Vals<V>& b)
+{
+    Vals<V> r;
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            unsigned long long d;
+            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair(a.v[j], a.v[j + 1])), "l"(pair(b.v[j], b.v[j + 1])));
+            split(d, r.v[j], r.v[j + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = a.v[j] * b.v[j];
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ float sum_of(Vals<V> a)
+{
+#pragma unroll
+    for (int h = V / 2; h >= 1; h >>= 1)
+#pragma unroll
+        for (int j = 0; j < h; ++j) a.v[j] += a.v[j + h];
+    return a.v[0];
+}
+
+template <int V> __device__ __forceinline__ Vals<V> values(const Pack<float, V>& p)
+{
+    Vals<V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = p.v[j];
+    return r;
+}
+template <int V> __device__ __forceinline__ Vals<V> values(const Pack<__nv_bfloat16, V>& p)
+{
+    Vals<V> r;
+    if constexpr (V % 2 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            unsigned w;
+            __builtin_memcpy(&w, &p.v[j], 4);
+            r.v[j] = __uint_as_float(w << 16);
+            r.v[j + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = to_f(p.v[j]);
+    }
+    return r;
+}
+template <int V> __device__ __forceinline__ Vals<V> values(const Pack<__half, V>& p)
+{
+    Vals<V> r;
+#pragma unroll
+    for (int j = 0; j < V; ++j) r.v[j] = to_f(p.v[j]);
+    return r;
+}
+// Rounds V values to the array's type, two to an instruction where it has one.
+template <class T, int V> __device__ __forceinline__ Pack<T, V> rounded(const Vals<V>& a)
+{
+    Pack<T, V> r;
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            if constexpr (__is_same(T, __nv_bfloat16)) {
+                const __nv_bfloat162 w = __floats2bfloat162_rn(a.v[j], a.v[j + 1]);
+                __builtin_memcpy(&r.v[j], &w, 4);
+            } else {
+                const __half2 w = __floats2half2_rn(a.v[j], a.v[j + 1]);
+                __builtin_memcpy(&r.v[j], &w, 4);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = from_f<T>(a.v[j]);
+    }
+    return r;
+}
+
 // ---- sums -------------------------------------------------------------------------------------------------------
 // Sum over `width` neighbouring lanes (a power of two); every lane has it.
-__device__ __forceinline__ float lanes_sum(float v, int width)
+__device__ __forceinline__ float lanes_sum(float v, int width = 32)
 {
-    for (int d = width >> 1; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1)
+        if (d < width) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
-__device__ __forceinline__ float lanes_max(float v, int width)
+__device__ __forceinline__ float lanes_max(float v, int width = 32)
 {
-    for (int d = width >> 1; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1)
+        if (d < width) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
     return v;
 }
+// Barrier of `threads` threads (whole warps) of the block; groups of one block use numbers of their own, 1 to 15.
+__device__ __forceinline__ void group_barrier(int number, int threads)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(number), "r"(threads) : "memory");
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float nan_f() { return __uint_as_float(0x7fffffffu); }
 
 // ---- the 8-bit checkpoint ---------------------------------------------------------------------------------------
 // Blocks of 32 consecutive values of a row or plane: one byte e stands for the step 2^(e - 127), a signed byte q for the value
@@ -100,46 +241,98 @@ __device__ __forceinline__ float lanes_max(float v, int width)
 // q = -128 marks an infinity or NaN and reads as NaN.  64 * 2^122 and (fp16) 64 * 2^10 would be infinite: the largest finite
 // values of a type are held to 63 steps.
 constexpr int kBlock = 32;
-constexpr unsigned kFiniteEnd = 0x7f800000u;      // magnitude bits from here on: infinity, NaN
 
-__device__ __forceinline__ unsigned magnitude_bits(float v)
-{
-    const unsigned b = __float_as_uint(v) & 0x7fffffffu;
-    return b < kFiniteEnd ? b : 0u;
-}
 // 127 * 2^k = 1.984375 * 2^(k + 6): the exponent field of the magnitude minus 6, one more if its fraction is above 0x7e0000.
-__device__ __forceinline__ unsigned step_exponent(unsigned largest_bits)
+__device__ __forceinline__ unsigned step_exponent(float largest)
 {
-    const int e = (int)((largest_bits + 0x1ffffu) >> 23) - 6;
+    const int e = (int)((__float_as_uint(largest) + 0x1ffffu) >> 23) - 6;
     return e < 1 ? 1u : (unsigned)e;
 }
 __device__ __forceinline__ float step_of(unsigned e) { return __uint_as_float(e << 23); }
 __device__ __forceinline__ float inverse_step(unsigned e) { return __uint_as_float((254u - e) << 23); }
-template <class T> __device__ __forceinline__ float most_steps(unsigned e)
+// Blocks for which rounding alone is not all: an infinity or NaN in them, or a largest value that rounds to 64 steps of a step too large.
+template <class T> __device__ __forceinline__ bool special(float largest)
 {
-    return e == 249u || (sizeof(T) == 2 && !__is_same(T, __nv_bfloat16) && e == 137u) ? 63.f : 127.f;
+    constexpr float last = sizeof(T) == 2 && !__is_same(T, __nv_bfloat16) ? 65024.f : 1.984375f * 0x1p127f;   // 127 of the last step that is not
+    return !(largest <= last);
 }
-// The byte q of a value: adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it in the low bits.
-__device__ __forceinline__ unsigned to_steps(float v, float inverse, float most)
+
+// The steps of V values whose block is spread over 32 / V neighbouring lanes (all lanes of the warp take part), and its exponent.
+// Adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it in the low byte.
+template <class T, int V> __device__ __forceinline__ Pack<unsigned char, V> to_steps(const Vals<V>& x, unsigned& e)
 {
-    const float s = fminf(fmaxf(v * inverse, -most), most) + 12582912.f;
-    return (__float_as_uint(v) & 0x7fffffffu) < kFiniteEnd ? __float_as_uint(s) & 0xffu : 0x80u;
-}
-// Values of the four bytes of a word.  A byte plus 128 in the low bits of 2^23 is the float 2^23 + q + 128.
-__device__ __forceinline__ void from_steps(unsigned word, float step, float (&out)[4])
-{
-    const unsigned u = word ^ 0x80808080u;
+    float big = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) out[j] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + j)) - 8388736.f) * step;
-    if ((u - 0x01010101u) & ~u & 0x80808080u) {             // a byte of u is 0
+    for (int j = 0; j < V; ++j) big = max_nan(big, fabsf(x.v[j]));
+    if constexpr (V == 1) big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));     // (a NaN's bits are above all)
+    else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (((word >> (8 * j)) & 0xffu) == 0x80u) out[j] = __uint_as_float(0x7fffffffu);
+        for (int d = kBlock / V / 2; d >= 1; d >>= 1) big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, d));
     }
+    Pack<unsigned char, V> q;
+    if (special<T>(big)) {
+        // every lane of the block is here: largest finite magnitude, then each value by itself
+        float finite = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) finite = fabsf(x.v[j]) < INFINITY ? fmaxf(finite, fabsf(x.v[j])) : finite;
+        const unsigned lanes = V == 1 ? 0xffffffffu : ((1u << (kBlock / V % 32)) - 1u) << (threadIdx.x & 31 & ~(kBlock / V - 1));
+        finite = __uint_as_float(__reduce_max_sync(lanes, __float_as_uint(finite)));
+        e = step_exponent(finite);
+        const float inverse = inverse_step(e), most = special<T>(finite) ? 63.f : 127.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float s = fminf(fmaxf(x.v[j] * inverse, -most), most) + 12582912.f;
+            q.v[j] = fabsf(x.v[j]) < INFINITY ? (unsigned char)__float_as_uint(s) : (unsigned char)0x80u;
+        }
+        return q;
+    }
+    e = step_exponent(big);
+    const Vals<V> s = fma(x, all<V>(inverse_step(e)), all<V>(12582912.f));
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            const unsigned lo = __byte_perm(__float_as_uint(s.v[j]), __float_as_uint(s.v[j + 1]), 0x0040);
+            const unsigned hi = __byte_perm(__float_as_uint(s.v[j + 2]), __float_as_uint(s.v[j + 3]), 0x0040);
+            const unsigned w = __byte_perm(lo, hi, 0x5410);
+            __builtin_memcpy(&q.v[j], &w, 4);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) q.v[j] = (unsigned char)__float_as_uint(s.v[j]);
+    }
+    return q;
 }
-__device__ __forceinline__ float from_step(unsigned char q, float step)
+
+// The steps as numbers: a byte plus 128 in the low bits of 2^23 is the float 2^23 + q + 128.  -128 becomes NaN.
+template <int V> __device__ __forceinline__ Vals<V> steps_of(const Pack<unsigned char, V>& q)
 {
-    return q == 0x80u ? __uint_as_float(0x7fffffffu) : (float)(signed char)q * step;
+    Vals<V> r;
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            unsigned w;
+            __builtin_memcpy(&w, &q.v[j], 4);
+            const unsigned u = w ^ 0x80808080u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r.v[j + k] = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7540 + k));
+        }
+        r = add(r, all<V>(-8388736.f));
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            unsigned w;
+            __builtin_memcpy(&w, &q.v[j], 4);
+            const unsigned u = w ^ 0x80808080u;
+            if ((u - 0x01010101u) & ~u & 0x80808080u) {          // a byte of u is 0
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (((u >> (8 * k)) & 0xffu) == 0u) r.v[j + k] = nan_f();
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = q.v[j] == 0x80u ? nan_f() : (float)(signed char)q.v[j];
+    }
+    return r;
 }
 
 // Where a checkpoint lies: q bytes of run r (a row or plane of `len` values) at r * pitch, its step bytes at steps + r * blocks.

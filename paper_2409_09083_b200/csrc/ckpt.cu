@@ -50,16 +50,8 @@ template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads)
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const long long e = first + i * 32 * V;
-                unsigned big = 0;
-#pragma unroll
-                for (int j = 0; j < V; ++j) big = max(big, magnitude_bits(to_f(raw[i].v[j])));
-#pragma unroll
-                for (int d = kBlock / V / 2; d >= 1; d >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
-                const unsigned ex = step_exponent(big);
-                const float inverse = inverse_step(ex), most = most_steps<T>(ex);
-                Pack<unsigned char, V> b;
-#pragma unroll
-                for (int j = 0; j < V; ++j) b.v[j] = (unsigned char)to_steps(to_f(raw[i].v[j]), inverse, most);
+                unsigned ex;
+                const Pack<unsigned char, V> b = to_steps<T, V>(values(raw[i]), ex);
                 if (e < a.ck.pitch) {
                     store_pack<unsigned char, V>(q + e, b);
                     if (e % kBlock == 0) steps[e / kBlock] = (unsigned char)ex;
@@ -77,23 +69,7 @@ template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads)
             for (int i = 0; i < kPer; ++i) {
                 const long long e = first + i * 32 * V;
                 if (e >= a.len) continue;
-                Pack<T, V> out;
-                const float step = step_of(ex[i]);
-                if constexpr (V % 4 == 0) {
-#pragma unroll
-                    for (int j = 0; j < V; j += 4) {
-                        unsigned w;
-                        __builtin_memcpy(&w, &b[i].v[j], 4);
-                        float f[4];
-                        from_steps(w, step, f);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) out.v[j + k] = from_f<T>(f[k]);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) out.v[j] = from_f<T>(from_step(b[i].v[j], step));
-                }
-                store_part<T, V>(x, e, 0, a.len, out);
+                store_part<T, V>(x, e, 0, a.len, rounded<T, V>(mul(steps_of(b[i]), all<V>(step_of(ex[i])))));
             }
         }
     }

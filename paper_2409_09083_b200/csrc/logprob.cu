@@ -48,8 +48,6 @@ struct LpArgs {
 enum { kStats = 0, kLoss = 1 };
 
 __device__ __forceinline__ float ex2(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
-__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ float nan_f() { return __uint_as_float(0x7fffffffu); }
 __device__ __forceinline__ float minus_inf() { return __uint_as_float(0xff800000u); }
 
 // Key of a value and its class; a NaN ranks as -infinity, -0 as 0.  Every key of a class is above 0.

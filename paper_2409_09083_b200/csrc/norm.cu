@@ -1,13 +1,13 @@
 // Channel norm, forward and backward (ftp_norm_forward, ftp_norm_backward).
 //
 // Both directions are bound by memory: forward reads x and writes y, backward reads x (or its checkpoint) and dy and writes dx.
-// So a row of values is read once and stays in registers between its statistics and its result, and a block takes rows until
-// none are left.  Two layouts: matrices (p = 1), where the threads of a group lie along the row, and maps (p > 1), where the
-// lanes of a warp lie along the pixels of a plane and groups of threads share out the channels.
+// So a row of values is read once and stays in registers between its statistics and its result.  Two layouts: matrices (p = 1), where
+// the threads of a group lie along the row, and maps (p > 1), where the lanes of a warp lie along the pixels of a plane and a thread holds
+// up to 32 channels of its pixels.
 //
-// The variance is the mean of (x - mean)^2 over values in registers, not E x^2 - mean^2.  dweight and dbias: a thread keeps the
-// same columns (channels) for all its rows and sums them in registers; each block writes one partial set and a second launch adds
-// the sets in a fixed order.
+// The variance is the mean of (x - mean)^2 over values in registers, not E x^2 - mean^2.  dweight and dbias: a thread (in maps: a lane)
+// keeps the same columns for all its rows and sums them in registers; each block writes one partial set and a second launch adds the
+// sets in a fixed order.
 #include "arrays.cuh"
 
 using namespace ftp;
@@ -32,161 +32,147 @@ struct NormArgs {
     int w_vec;                   // weight and bias are 16-byte aligned
 };
 
-constexpr int kRowThreads = 256;       // matrices: threads of a block whose rows are shorter than that many vectors
-constexpr int kMapThreads = 256;
-
-// Adds over the `tpr` threads of a group; tpr a power of two, groups within a warp or a whole number of warps.  `red`: a float a warp,
-// not read or written by anyone else until another barrier has passed.
-template <int K> __device__ __forceinline__ void group_sum(float (&v)[K], int tpr, float* red)
+// Adds over the `tpr` threads of a group; tpr a power of two, groups within a warp or a whole number of warps with barrier `number`.
+// `red`: K floats a warp, not read or written by anyone else until the group has passed another barrier.
+template <int K> __device__ __forceinline__ void group_sum(float (&v)[K], int tpr, int number, float* red)
 {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = lanes_sum(v[k], tpr < 32 ? tpr : 32);
+    for (int k = 0; k < K; ++k) v[k] = lanes_sum(v[k], tpr);
     if (tpr <= 32) return;
     const int warp = threadIdx.x >> 5, per = tpr >> 5, first = warp & ~(per - 1);
     if ((threadIdx.x & 31) == 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k) red[warp * K + k] = v[k];
     }
-    __syncthreads();
+    group_barrier(number, tpr);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float s = 0.f;
-        for (int i = 0; i < per; ++i) s += red[(first + i) * K + k];
-        v[k] = s;
-    }
+    for (int k = 0; k < K; ++k) v[k] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < per; ++i)
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] += red[(first + i) * K + k];
 }
 
-// weight or bias of columns [col, col + V) (null: `none`); columns outside [0, c) read as `none`.
-template <int V> __device__ __forceinline__ void load_cols(const float* w, int col, int c, bool vec, float none, float (&out)[V])
+// weight or bias of columns [col, col + V) (null: `none`); columns outside [0, c) read as `none`.  FAST: there, whole and aligned.
+template <bool FAST, int V> __device__ __forceinline__ void load_cols(const float* w, int col, int c, float none, float* out)
 {
-    if (w && vec && V % 4 == 0 && col >= 0 && (col & 3) == 0 && col + V <= c) {
+    if constexpr (FAST) {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
             const float4 q = __ldg(reinterpret_cast<const float4*>(w + col + j));
-            out[j] = q.x; out[(j + 1) % V] = q.y; out[(j + 2) % V] = q.z; out[(j + 3) % V] = q.w;
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j) out[j] = w && col + j >= 0 && col + j < c ? __ldg(w + col + j) : none;
-}
-
-// The checkpoint's bytes of V values whose block is spread over 32 / V neighbouring lanes (all lanes take part).
-template <class T, int V> __device__ __forceinline__ Pack<unsigned char, V> make_steps(const Pack<T, V>& a, unsigned& e)
-{
-    unsigned big = 0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) big = max(big, magnitude_bits(to_f(a.v[j])));
-#pragma unroll
-    for (int d = kBlock / V / 2; d >= 1; d >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, d));
-    e = step_exponent(big);
-    const float inverse = inverse_step(e), most = most_steps<T>(e);
-    Pack<unsigned char, V> q;
-#pragma unroll
-    for (int j = 0; j < V; ++j) q.v[j] = (unsigned char)to_steps(to_f(a.v[j]), inverse, most);
-    return q;
-}
-
-template <int V> __device__ __forceinline__ void read_steps(const Pack<unsigned char, V>& q, float step, float (&out)[V])
-{
-    if constexpr (V % 4 == 0) {
-#pragma unroll
-        for (int j = 0; j < V; j += 4) {
-            unsigned w;
-            __builtin_memcpy(&w, &q.v[j], 4);
-            float f[4];
-            from_steps(w, step, f);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) out[j + k] = f[k];
+            out[j] = q.x; out[j + 1] = q.y; out[j + 2] = q.z; out[j + 3] = q.w;
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = from_step(q.v[j], step);
+        for (int j = 0; j < V; ++j) out[j] = w && (unsigned)(col + j) < (unsigned)c ? __ldg(w + col + j) : none;
     }
 }
 
-// What a row's x is read as: packs of the array, or steps of the checkpoint.
+// x of a row as it is read: packs of the array, or steps of the checkpoint.  hats() gives (x - mean) rstd from rstd and -mean rstd:
+// one multiply-add, off by no more than the rounding of mean itself; q (step rstd) is as exact, the step being a power of two.
 template <class T, int V, bool CK> struct Raw;
 template <class T, int V> struct Raw<T, V, false> {
     Pack<T, V> a;
-    __device__ __forceinline__ void values(float (&out)[V]) const
-    {
-#pragma unroll
-        for (int j = 0; j < V; ++j) out[j] = to_f(a.v[j]);
-    }
+    __device__ __forceinline__ void clear() { a = zero_pack<T, V>(); }
+    __device__ __forceinline__ Vals<V> hats(float rstd, float shift) const { return fma(values(a), all<V>(rstd), all<V>(shift)); }
+    __device__ __forceinline__ Vals<V> hats(const Vals<V>& rstd, const Vals<V>& shift) const { return fma(values(a), rstd, shift); }
 };
 template <class T, int V> struct Raw<T, V, true> {
     Pack<unsigned char, V> q;
-    unsigned char e;
-    __device__ __forceinline__ void values(float (&out)[V]) const { read_steps<V>(q, step_of(e), out); }
+    unsigned e;
+    __device__ __forceinline__ void clear()
+    {
+        e = 1;
+#pragma unroll
+        for (int j = 0; j < V; ++j) q.v[j] = 0;
+    }
+    __device__ __forceinline__ Vals<V> hats(float rstd, float shift) const { return fma(steps_of(q), all<V>(rstd * step_of(e)), all<V>(shift)); }
+    __device__ __forceinline__ Vals<V> hats(const Vals<V>& rstd, const Vals<V>& shift) const { return fma(steps_of(q), mul(rstd, all<V>(step_of(e))), shift); }
 };
 
 // ---- matrices ---------------------------------------------------------------------------------------------------
-// A group of `tpr` threads holds a row as VPT vectors of V values a thread: vector i * tpr + t.  SHIFT: rows start at any
-// multiple of the value's size, and the vectors lie on the 16-byte grid below the row's start (x and y the same distance above
-// it); then column = place - o.  With V = 1 any alignment goes.
-template <class T, int V, int VPT, bool SHIFT, bool CK>
-__global__ void __launch_bounds__(1024) norm_fwd_rows_kernel(NormArgs a, int tpr)
+// A group of `tpr` threads holds a row as VPT vectors of V values a thread: vector i * tpr + t.  FAST: every vector lies in the row as a
+// whole, and weight and bias are there and aligned.  SHIFT: rows start at any multiple of the value's size, and the vectors lie on
+// the 16-byte grid below the row's start (x and y the same distance above it); then column = place - o.  With V = 1 any alignment goes.
+enum { kFast, kEdge, kShift };
+
+template <class T, int V, int VPT, int FORM, bool CK, int MOST>
+__global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_rows_kernel(NormArgs a, int tpr)
 {
+    constexpr bool kWhole = FORM == kFast || V == 1;
+    constexpr int E = V * VPT;
     __shared__ float red[2][32];
     previous_launches();
-    const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1);
+    const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = threadIdx.x / tpr;
+    const float inv_c = 1.f / (float)a.c;
     for (long long row0 = (long long)blockIdx.x * per; row0 < a.rows; row0 += (long long)gridDim.x * per) {
-        const long long row = row0 + threadIdx.x / tpr;
+        const long long row = row0 + group;
         const bool live = row < a.rows;
         const T* xr = static_cast<const T*>(a.x) + row * a.x_stride;
-        T* yr = static_cast<T*>(a.out) + row * a.out_stride;
-        const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(xr) / sizeof(T)) & (V - 1)) : 0;
+        const int o = FORM == kShift ? (int)((reinterpret_cast<uintptr_t>(xr) / sizeof(T)) & (V - 1)) : 0;
         const int hi = live ? o + a.c : 0;
-        xr -= o; yr -= o;
+        xr -= o;
         Pack<T, V> raw[VPT];
-        float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            raw[i] = e < hi ? load_part<T, V>(xr, e, o, hi) : zero_pack<T, V>();
+            raw[i] = zero_pack<T, V>();
+            if (e < hi) raw[i] = kWhole ? load_pack<T, V>(xr + e) : load_part<T, V>(xr, e, o, hi);
         }
+        Vals<E> x;
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
+        for (int i = 0; i < VPT; ++i) {
+            const Vals<V> v = values(raw[i]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[0] += to_f(raw[i].v[j]);
-        group_sum<1>(s, tpr, red[0]);
-        const float mean = s[0] / (float)a.c;
-        float q[1] = {0.f};
+            for (int j = 0; j < V; ++j) x.v[i * V + j] = v.v[j];
+        }
+        float s[1] = {sum_of(x)};
+        group_sum<1>(s, tpr, group + 1, red[0]);
+        const float mean = a.c == 1 ? s[0] : s[0] * inv_c;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
+            const float minus = e < hi ? -mean : 0.f;           // (a vector that is not there stays 0)
+            Vals<V> v;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = to_f(raw[i].v[j]) - mean;
-                if (e + j >= o && e + j < hi) q[0] = fmaf(d, d, q[0]);
+            for (int j = 0; j < V; ++j) v.v[j] = x.v[i * V + j];
+            v = add(v, all<V>(minus));
+            if (!kWhole && (e < o || e + V > hi)) {             // nor places before or behind the row
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (e + j < o || e + j >= hi) v.v[j] = 0.f;
             }
+#pragma unroll
+            for (int j = 0; j < V; ++j) x.v[i * V + j] = v.v[j];
         }
-        group_sum<1>(q, tpr, red[1]);
-        const float rstd = 1.f / sqrtf(q[0] / (float)a.c + a.eps);
+        s[0] = sum_of(mul(x, x));
+        group_sum<1>(s, tpr, group + 1, red[1]);
+        const float rstd = 1.f / sqrtf(s[0] * inv_c + a.eps);
         if (live && t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
+        T* yr = static_cast<T*>(a.out) + row * a.out_stride - o;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
             if (CK) {
                 unsigned ex;
-                const Pack<unsigned char, V> st = make_steps<T, V>(raw[i], ex);
+                const Pack<unsigned char, V> st = to_steps<T, V>(values(raw[i]), ex);
                 if (live && e < a.ck.pitch) {
                     store_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e, st);
                     if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
                 }
             }
             if (e < hi) {
-                float w[V], b[V];
-                load_cols<V>(a.weight, e - o, a.c, a.w_vec, 1.f, w);
-                load_cols<V>(a.bias, e - o, a.c, a.w_vec, 0.f, b);
-                Pack<T, V> y;
+                Vals<V> w, b, v;
+                load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v);
+                load_cols<FORM == kFast, V>(a.bias, e - o, a.c, 0.f, b.v);
 #pragma unroll
-                for (int j = 0; j < V; ++j) y.v[j] = from_f<T>(fmaf((to_f(raw[i].v[j]) - mean) * rstd, w[j], b[j]));
-                store_part<T, V>(yr, e, o, hi, y);
+                for (int j = 0; j < V; ++j) v.v[j] = x.v[i * V + j];
+                const Pack<T, V> y = rounded<T, V>(fma(mul(v, all<V>(rstd)), w, b));
+                if (kWhole) store_pack<T, V>(yr + e, y);
+                else store_part<T, V>(yr, e, o, hi, y);
             }
         }
     }
@@ -202,10 +188,10 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
         T* yr = static_cast<T*>(a.out) + row * a.out_stride;
         float s[1] = {0.f}, q[1] = {0.f};
         for (int e = threadIdx.x; e < a.c; e += 1024) s[0] += to_f(xr[e]);
-        group_sum<1>(s, 1024, red[0]);
+        group_sum<1>(s, 1024, 1, red[0]);
         const float mean = s[0] / (float)a.c;
         for (int e = threadIdx.x; e < a.c; e += 1024) { const float d = to_f(xr[e]) - mean; q[0] = fmaf(d, d, q[0]); }
-        group_sum<1>(q, 1024, red[1]);
+        group_sum<1>(q, 1024, 1, red[1]);
         const float rstd = 1.f / sqrtf(q[0] / (float)a.c + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -217,7 +203,7 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
             if (e < a.c) v.v[0] = xr[e];
             if (CK) {
                 unsigned ex;
-                const Pack<unsigned char, 1> st = make_steps<T, 1>(v, ex);
+                const Pack<unsigned char, 1> st = to_steps<T, 1>(values(v), ex);
                 a.ck.q[row * a.ck.pitch + e] = st.v[0];
                 if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
             }
@@ -227,85 +213,105 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
     }
 }
 
-// Backward pass of matrices; the same spread of a row over a group.  A thread's columns are the same in every row, so dweight and
-// dbias of its columns add up in registers over all rows of the block.
-template <class T, int V, int VPT, bool CK>
-__global__ void __launch_bounds__(V* VPT >= 16 ? 512 : 1024) norm_bwd_rows_kernel(NormArgs a, int tpr)
+// Backward pass of matrices; the same spread of a row over a group, a block's groups (each with a barrier of its own) taking rows in
+// turn.  A thread's columns are the same in every row, so dweight and dbias of its columns add up in registers over all rows of the block.
+// The next row's values are on their way while a row is summed: with one block of 512 threads an SM, whose 128 registers a thread hold the
+// sums, 32 KB are always in flight.
+template <class T, int V, int VPT, bool CK> struct RowIn {
+    Raw<T, V, CK> x[VPT];
+    Pack<T, V> dy[VPT];
+    float mean, rstd;
+};
+template <class T, int V, int VPT, bool FAST, bool CK>
+__device__ __forceinline__ void load_row(const NormArgs& a, long long row, int tpr, int t, RowIn<T, V, VPT, CK>& in)
 {
+    constexpr bool kWhole = FAST || V == 1;
+    const bool live = row < a.rows;
+    const int c = live ? a.c : 0;
+    const T* dyr = static_cast<const T*>(a.dy) + row * a.dy_stride;
+    const T* xr = static_cast<const T*>(a.x) + row * a.x_stride;
+    const unsigned char* qr = a.ck.q + row * a.ck.pitch;
+    const unsigned char* er = a.ck.steps + row * a.ck.blocks;
+    in.mean = in.rstd = 0.f;
+    if (live) { in.mean = a.mean[row]; in.rstd = a.rstd[row]; }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int e = (i * tpr + t) * V;
+        in.dy[i] = zero_pack<T, V>();
+        in.x[i].clear();
+        if (e < c) {
+            in.dy[i] = kWhole ? load_pack<T, V>(dyr + e) : load_part<T, V>(dyr, e, 0, c);
+            if constexpr (CK) {
+                in.x[i].q = load_pack<unsigned char, V>(qr + e);
+                in.x[i].e = er[e / kBlock];
+            } else in.x[i].a = kWhole ? load_pack<T, V>(xr + e) : load_part<T, V>(xr, e, 0, c);
+        }
+    }
+}
+
+template <class T, int V, int VPT, bool FAST, bool CK>
+__global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int tpr)
+{
+    constexpr bool kWhole = FAST || V == 1;
+    constexpr int E = V * VPT;
     extern __shared__ float smem[];                    // a set of columns per group, to add the groups of the block
-    __shared__ float red[2][64];
+    __shared__ float red[2][32];
     previous_launches();
-    const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1);
+    next_launch();
+    const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = threadIdx.x / tpr;
     const float inv_c = 1.f / (float)a.c;
-    float dw[VPT][V], db[VPT][V];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = 0.f;
+    Vals<E> dw = all<E>(0.f), db = all<E>(0.f);
+    const long long step = (long long)gridDim.x * per;
+    long long row = (long long)blockIdx.x * per + group;
+    RowIn<T, V, VPT, CK> next;
+    load_row<T, V, VPT, FAST, CK>(a, row, tpr, t, next);
     int turn = 0;
-    for (long long row0 = (long long)blockIdx.x * per; row0 < a.rows; row0 += (long long)gridDim.x * per, turn ^= 1) {
-        const long long row = row0 + threadIdx.x / tpr;
-        const bool live = row < a.rows;
-        const int c = live ? a.c : 0;
-        Raw<T, V, CK> x[VPT];
-        Pack<T, V> dy[VPT];
+    // (groups narrower than a warp stay together: a warp goes on until none of its rows is left)
+    for (long long first = (long long)blockIdx.x * per + (tpr < 32 ? (threadIdx.x & ~31) / tpr : group); first < a.rows; first += step, turn ^= 1) {
+        const float rstd = next.rstd, shift = -next.mean * next.rstd;
+        Vals<E> d, g, hat;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            if (e < c) {
-                dy[i] = load_part<T, V>(static_cast<const T*>(a.dy) + row * a.dy_stride, e, 0, c);
-                if constexpr (CK) {
-                    x[i].q = load_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e);
-                    x[i].e = a.ck.steps[row * a.ck.blocks + e / kBlock];
-                } else x[i].a = load_part<T, V>(static_cast<const T*>(a.x) + row * a.x_stride, e, 0, c);
-            }
+            const Vals<V> di = values(next.dy[i]), hi = next.x[i].hats(rstd, shift);
+            Vals<V> w = all<V>(0.f);
+            if (e < a.c) load_cols<FAST, V>(a.weight, e, a.c, 1.f, w.v);
+            const Vals<V> gi = mul(di, w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) { d.v[i * V + j] = di.v[j]; g.v[i * V + j] = gi.v[j]; hat.v[i * V + j] = hi.v[j]; }
         }
-        const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
-        float s[2] = {0.f, 0.f};
+        const long long here = row;
+        row += step;
+        load_row<T, V, VPT, FAST, CK>(a, row, tpr, t, next);
+        dw = fma(d, hat, dw);
+        db = add(db, d);
+        float s[2] = {sum_of(g), sum_of(mul(g, hat))};
+        group_sum<2>(s, tpr, group + 1, red[turn]);
+        if (a.out && here < a.rows) {
+            const Vals<E> dx = fma(hat, all<E>(-s[1] * inv_c * rstd), fma(g, all<E>(rstd), all<E>(-s[0] * inv_c * rstd)));
+            T* out = static_cast<T*>(a.out) + here * a.out_stride;
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int e = (i * tpr + t) * V;
-            if (e >= c) continue;
-            float xv[V], w[V];
-            x[i].values(xv);
-            load_cols<V>(a.weight, e, a.c, a.w_vec, 1.f, w);
+            for (int i = 0; i < VPT; ++i) {
+                const int e = (i * tpr + t) * V;
+                Vals<V> v;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = to_f(dy[i].v[j]), hat = (xv[j] - mean) * rstd, g = d * w[j];
-                if (e + j < c) { s[0] += g; s[1] = fmaf(g, hat, s[1]); }
-                dw[i][j] = fmaf(d, hat, dw[i][j]);
-                db[i][j] += d;
+                for (int j = 0; j < V; ++j) v.v[j] = dx.v[i * V + j];
+                if (e < a.c) {
+                    if (kWhole) store_pack<T, V>(out + e, rounded<T, V>(v));
+                    else store_part<T, V>(out, e, 0, a.c, rounded<T, V>(v));
+                }
             }
-        }
-        group_sum<2>(s, tpr, red[turn]);
-        if (!a.out) continue;
-        const float m0 = s[0] * inv_c, m1 = s[1] * inv_c;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int e = (i * tpr + t) * V;
-            if (e >= c) continue;
-            float xv[V], w[V];
-            x[i].values(xv);
-            load_cols<V>(a.weight, e, a.c, a.w_vec, 1.f, w);
-            Pack<T, V> dx;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float hat = (xv[j] - mean) * rstd;
-                dx.v[j] = from_f<T>((fmaf(to_f(dy[i].v[j]), w[j], -m0) - hat * m1) * rstd);
-            }
-            store_part<T, V>(static_cast<T*>(a.out) + row * a.out_stride, e, 0, c, dx);
         }
     }
     if (!a.partials) return;
-    next_launch();
-    const int width = tpr * VPT * V;
+    const int width = tpr * E;
     float* set = a.partials + (long long)blockIdx.x * 2 * a.c;
     for (int k = 0; k < 2; ++k) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
-            for (int j = 0; j < V; ++j) smem[(threadIdx.x / tpr) * width + (i * tpr + t) * V + j] = k ? db[i][j] : dw[i][j];
+            for (int j = 0; j < V; ++j) smem[group * width + (i * tpr + t) * V + j] = k ? db.v[i * V + j] : dw.v[i * V + j];
         __syncthreads();
         for (int e = threadIdx.x; e < a.c; e += blockDim.x) {
             float s = 0.f;
@@ -329,14 +335,20 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_lon
         const unsigned char* qr = a.ck.q + row * a.ck.pitch;
         const unsigned char* er = a.ck.steps + row * a.ck.blocks;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        auto hat_of = [&](int e) { return ((CK ? from_step(qr[e], step_of(er[e / kBlock])) : to_f(xr[e])) - mean) * rstd; };
+        const float shift = -mean * rstd;
+        auto hat_of = [&](int e) {
+            Raw<T, 1, CK> r;
+            if constexpr (CK) { r.q.v[0] = qr[e]; r.e = er[e / kBlock]; }
+            else r.a.v[0] = xr[e];
+            return r.hats(rstd, shift).v[0];
+        };
         float s[2] = {0.f, 0.f};
         for (int e = threadIdx.x; e < a.c; e += 1024) {
             const float g = to_f(dyr[e]) * (a.weight ? a.weight[e] : 1.f);
             s[0] += g;
             s[1] = fmaf(g, hat_of(e), s[1]);
         }
-        group_sum<2>(s, 1024, red[turn]);
+        group_sum<2>(s, 1024, 1, red[turn]);
         const float m0 = s[0] * inv_c, m1 = s[1] * inv_c;
         const bool first = row == blockIdx.x;
         for (int e = threadIdx.x; e < a.c; e += 1024) {
@@ -353,289 +365,404 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_lon
 }
 
 // ---- maps -------------------------------------------------------------------------------------------------------
-// A tile is lp * V pixels of one sample with all channels: lane l < lp of a group of lp threads has pixels l * V .. of
-// channels g, g + groups, ...  (CPT of them in registers, or any number if CPT is 0, then read again for every pass).
-struct Tile { long long n; int px; bool live; long long row; };
+// A tile is 32 V pixels of one sample with all channels: a lane has V pixels (4 bytes of them, or one value), and the `share` warps of
+// a group split the channels, `per` <= CPT to a warp, which stay in registers.  A block holds one or more groups.  With up to 32 channels
+// a warp works alone, without a barrier.
+struct Tile { long long n, row; int px, first, count; bool live; };
 
-__device__ __forceinline__ Tile tile_of(const NormArgs& a, long long tile, int tiles, int pixels, int at)
+__device__ __forceinline__ Tile tile_of(const NormArgs& a, long long tile, int tiles, int pixels, int at, int first, int per)
 {
     Tile t;
     t.n = tile / tiles;
     t.px = (int)(tile - t.n * tiles) * pixels + at;
     t.live = t.px < a.p;
     t.row = t.n * a.p + t.px;
+    t.first = first;
+    t.count = min(per, a.c - first);
     return t;
 }
 
-// Sums over the channels of each pixel: over the lanes of a warp that share pixels, then over the warps.  `red`: [warps][pixels * K].
-template <int K, int V> __device__ __forceinline__ void pixel_sum(float (&v)[K][V], int lp, float* red)
+// Adds K values of each pixel over the `share` warps of a group, in their order.
+template <int K, int V> __device__ __forceinline__ void pixel_sum(Vals<V> (&v)[K], int share, int number, float* red)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    if (share == 1) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp & ~(share - 1);
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            for (int d = 16; d >= lp; d >>= 1) v[k][j] += __shfl_xor_sync(0xffffffffu, v[k][j], d);
-    if (lane < lp) {
+        for (int j = 0; j < V; ++j) red[((warp * K + k) * V + j) * 32 + lane] = v[k].v[j];
+    group_barrier(number, share * 32);
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = all<V>(0.f);
+#pragma unroll 4
+    for (int w = 0; w < share; ++w)
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) red[((warp * K + k) * V + j) * lp + lane] = v[k][j];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float s = 0.f;
-            for (int w = 0; w < warps; ++w) s += red[((w * K + k) * V + j) * lp + (lane & (lp - 1))];
-            v[k][j] = s;
-        }
+            for (int j = 0; j < V; ++j) v[k].v[j] += red[(((first + w) * K + k) * V + j) * 32 + lane];
 }
 
-template <class T, int V, int CPT, bool CK>
-__global__ void __launch_bounds__(512) norm_fwd_map_kernel(NormArgs a, int lp, int tiles)
+// Bytes from a place of channel 0 to the same place of channel i: one wide multiply-add.
+__device__ __forceinline__ const char* plane(const char* base, unsigned bytes, int i) { return base + (unsigned long long)bytes * (unsigned)i; }
+__device__ __forceinline__ char* plane(char* base, unsigned bytes, int i) { return base + (unsigned long long)bytes * (unsigned)i; }
+
+// Weight and bias of all channels, in shared memory.
+__device__ __forceinline__ void stage_cols(const NormArgs& a, float2* wb)
 {
-    extern __shared__ float smem[];
-    previous_launches();
-    const int l = threadIdx.x & (lp - 1), g = threadIdx.x / lp, groups = blockDim.x / lp;
-    const int red = (blockDim.x >> 5) * lp * V;
-    const int slots = CPT ? CPT : (a.c + groups - 1) / groups;
-    for (long long tile = blockIdx.x; tile < a.n * tiles; tile += gridDim.x) {
-        const Tile t = tile_of(a, tile, tiles, lp * V, l * V);
-        const T* xt = static_cast<const T*>(a.x) + t.n * a.x_stride + t.px;
-        T* yt = static_cast<T*>(a.out) + t.n * a.out_stride + t.px;
-        auto load = [&](int i) {
-            const int ch = g + i * groups;
-            return t.live && ch < a.c ? load_pack<T, V>(xt + (long long)ch * a.p) : zero_pack<T, V>();
-        };
-        Pack<T, V> raw[CPT ? CPT : 1];
-        float s[1][V], q[1][V];
+    for (int i = threadIdx.x; i < a.c; i += blockDim.x) wb[i] = make_float2(a.weight ? a.weight[i] : 1.f, a.bias ? a.bias[i] : 0.f);
+    __syncthreads();
+}
+
+// FULL: all CPT channels and all pixels of the tile are there, which spares four tests for every value.
+template <class T, int V, int CPT, bool CK, bool FULL>
+__device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, int share, int number, float* red, int half, const float2* wb)
+{
+    const int count = FULL ? CPT : t.count;
+    const bool live = FULL || t.live;
+    const unsigned bytes = (unsigned)a.p * sizeof(T);
+    const float inv_c = 1.f / (float)a.c;
+    const char* xt = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + t.n * a.x_stride + (long long)t.first * a.p + t.px);
+    char* yt = reinterpret_cast<char*>(static_cast<T*>(a.out) + t.n * a.out_stride + (long long)t.first * a.p + t.px);
+    Pack<T, V> raw[CPT];
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[0][j] = q[0][j] = 0.f;
-        if constexpr (CPT > 0) {
+    for (int i = 0; i < CPT; ++i) {
+        if (!FULL) raw[i] = zero_pack<T, V>();
+        if (i < count && live) raw[i] = load_pack<T, V>(reinterpret_cast<const T*>(plane(xt, bytes, i)));
+    }
+    Vals<V> s[1] = {all<V>(0.f)};
 #pragma unroll
-            for (int i = 0; i < CPT; ++i) raw[i] = load(i);
+    for (int i = 0; i < CPT; ++i) s[0] = add(s[0], values(raw[i]));
+    pixel_sum<1, V>(s, share, number, red);
+    const Vals<V> mean = a.c == 1 ? s[0] : mul(s[0], all<V>(inv_c)), minus = mul(mean, all<V>(-1.f));
+    s[0] = all<V>(0.f);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i)
+        if (i < count) { const Vals<V> d = add(values(raw[i]), minus); s[0] = fma(d, d, s[0]); }
+    pixel_sum<1, V>(s, share, number, red + half);
+    Vals<V> rstd;
+#pragma unroll
+    for (int j = 0; j < V; ++j) rstd.v[j] = 1.f / sqrtf(s[0].v[j] * inv_c + a.eps);
+    if (live && t.first == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (a.mean) a.mean[t.row + j] = mean.v[j];
+            if (a.rstd) a.rstd[t.row + j] = rstd.v[j];
         }
-        auto sum = [&](const Pack<T, V>& r) {
+    }
+    const long long run = t.n * a.c + t.first;
+    char* qt = reinterpret_cast<char*>(a.ck.q + run * a.ck.pitch + t.px);
+    unsigned char* et = a.ck.steps + run * a.ck.blocks + t.px / kBlock;
 #pragma unroll
-            for (int j = 0; j < V; ++j) s[0][j] += to_f(r.v[j]);
-        };
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) sum(raw[i]);
-        } else
-            for (int i = 0; i < slots; ++i) sum(load(i));
-        pixel_sum<1, V>(s, lp, smem);
-        float mean[V], rstd[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) mean[j] = s[0][j] / (float)a.c;
-        auto square = [&](const Pack<T, V>& r, int i) {
-            if (g + i * groups >= a.c) return;
-#pragma unroll
-            for (int j = 0; j < V; ++j) { const float d = to_f(r.v[j]) - mean[j]; q[0][j] = fmaf(d, d, q[0][j]); }
-        };
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) square(raw[i], i);
-        } else
-            for (int i = 0; i < slots; ++i) square(load(i), i);
-        pixel_sum<1, V>(q, lp, smem + red);
-#pragma unroll
-        for (int j = 0; j < V; ++j) rstd[j] = 1.f / sqrtf(q[0][j] / (float)a.c + a.eps);
-        if (t.live && g == 0) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (a.mean) a.mean[t.row + j] = mean[j];
-                if (a.rstd) a.rstd[t.row + j] = rstd[j];
+    for (int i = 0; i < CPT; ++i) {
+        if (i >= count) continue;
+        if (CK) {
+            unsigned ex;
+            const Pack<unsigned char, V> st = to_steps<T, V>(values(raw[i]), ex);
+            if (FULL || t.px < a.ck.pitch) {
+                store_pack<unsigned char, V>(reinterpret_cast<unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)), st);
+                if (t.px % kBlock == 0) et[(unsigned long long)(unsigned)a.ck.blocks * i] = (unsigned char)ex;
             }
         }
-        auto finish = [&](const Pack<T, V>& r, int i) {
-            const int ch = g + i * groups;
+        if (live) {
+            const float2 c = wb[t.first + i];
+            store_pack<T, V>(reinterpret_cast<T*>(plane(yt, bytes, i)),
+                             rounded<T, V>(fma(add(values(raw[i]), minus), mul(rstd, all<V>(c.x)), all<V>(c.y))));
+        }
+    }
+}
+
+template <class T, int V, int CPT, bool CK, int MOST>
+__global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_map_kernel(NormArgs a, int share, int per, int tiles)
+{
+    extern __shared__ float smem[];                      // weight and bias, then [2][warps][V * 32]
+    previous_launches();
+    float2* wb = reinterpret_cast<float2*>(smem);
+    float* red = smem + 2 * a.c;
+    stage_cols(a, wb);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / share, groups = (blockDim.x >> 5) / share;
+    for (long long tile = (long long)blockIdx.x * groups + group; tile < a.n * tiles; tile += (long long)gridDim.x * groups) {
+        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, (warp & (share - 1)) * per, per);
+        if (t.count == CPT && t.px - lane * V + 32 * V <= a.p) norm_fwd_tile<T, V, CPT, CK, true>(a, t, share, group + 1, red, blockDim.x * V, wb);
+        else norm_fwd_tile<T, V, CPT, CK, false>(a, t, share, group + 1, red, blockDim.x * V, wb);
+    }
+}
+
+// More channels than registers hold: three passes over the tile, the second and third from L2.
+template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_fwd_long_map_kernel(NormArgs a, int tiles)
+{
+    __shared__ float red[2][512 * V];
+    previous_launches();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    for (long long tile = blockIdx.x; tile < a.n * tiles; tile += gridDim.x) {
+        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, 0, a.c);
+        const T* xt = static_cast<const T*>(a.x) + t.n * a.x_stride + t.px;
+        T* yt = static_cast<T*>(a.out) + t.n * a.out_stride + t.px;
+        auto load = [&](int ch) { return t.live ? values(load_pack<T, V>(xt + (long long)ch * a.p)) : all<V>(0.f); };
+        Vals<V> s[1] = {all<V>(0.f)};
+        for (int ch = warp; ch < a.c; ch += warps) s[0] = add(s[0], load(ch));
+        pixel_sum<1, V>(s, warps, 1, red[0]);
+        Vals<V> mean, rstd;
+#pragma unroll
+        for (int j = 0; j < V; ++j) mean.v[j] = s[0].v[j] / (float)a.c;
+        const Vals<V> minus = mul(mean, all<V>(-1.f));
+        s[0] = all<V>(0.f);
+        for (int ch = warp; ch < a.c; ch += warps) { const Vals<V> d = add(load(ch), minus); s[0] = fma(d, d, s[0]); }
+        pixel_sum<1, V>(s, warps, 1, red[1]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) rstd.v[j] = 1.f / sqrtf(s[0].v[j] / (float)a.c + a.eps);
+        if (t.live && warp == 0) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (a.mean) a.mean[t.row + j] = mean.v[j];
+                if (a.rstd) a.rstd[t.row + j] = rstd.v[j];
+            }
+        }
+        for (int ch = warp; ch < a.c; ch += warps) {
+            const Vals<V> x = load(ch);
             if (CK) {
                 unsigned ex;
-                const Pack<unsigned char, V> st = make_steps<T, V>(r, ex);
-                if (ch < a.c && t.px < a.ck.pitch) {
+                const Pack<unsigned char, V> st = to_steps<T, V>(x, ex);
+                if (t.px < a.ck.pitch) {
                     const long long run = t.n * a.c + ch;
                     store_pack<unsigned char, V>(a.ck.q + run * a.ck.pitch + t.px, st);
                     if (t.px % kBlock == 0) a.ck.steps[run * a.ck.blocks + t.px / kBlock] = (unsigned char)ex;
                 }
             }
-            if (t.live && ch < a.c) {
+            if (t.live) {
                 const float w = a.weight ? __ldg(a.weight + ch) : 1.f, b = a.bias ? __ldg(a.bias + ch) : 0.f;
-                Pack<T, V> y;
-#pragma unroll
-                for (int j = 0; j < V; ++j) y.v[j] = from_f<T>(fmaf((to_f(r.v[j]) - mean[j]) * rstd[j], w, b));
-                store_pack<T, V>(yt + (long long)ch * a.p, y);
+                store_pack<T, V>(yt + (long long)ch * a.p, rounded<T, V>(fma(mul(add(x, minus), rstd), all<V>(w), all<V>(b))));
             }
-        };
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) finish(raw[i], i);
-        } else
-            for (int i = 0; i < slots; ++i) finish(load(i), i);
+        }
     }
 }
 
-template <class T, int V, int CPT, bool CK>
-__global__ void __launch_bounds__(512) norm_bwd_map_kernel(NormArgs a, int lp, int tiles)
+// Sums over the 32 lanes of N values a lane: lane l < N ends with the sum of value l.  Halving: at each step a lane gives half of its
+// values to the lane across and keeps the other half, N - 1 exchanges in all instead of 5 N.
+template <int N> __device__ __forceinline__ float across_lanes(float (&v)[N], int lane)
 {
-    extern __shared__ float smem[];
-    previous_launches();
-    const int l = threadIdx.x & (lp - 1), g = threadIdx.x / lp, groups = blockDim.x / lp;
-    const int red = (blockDim.x >> 5) * lp * V * 2;
-    const int slots = CPT ? CPT : (a.c + groups - 1) / groups;
-    const float inv_c = 1.f / (float)a.c;
-    constexpr int R = CPT ? CPT : 1;
-    float dw[R], db[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) dw[i] = db[i] = 0.f;
+    for (int h = N / 2; h >= 1; h >>= 1) {
+        const bool up = lane & h;
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, h);
+        }
+    }
+    float s = v[0];
+#pragma unroll
+    for (int d = 16; d >= N; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    return s;
+}
+
+template <class T, int V, bool CK>
+__device__ __forceinline__ void load_map(const NormArgs& a, const Tile& t, int ch, Raw<T, V, CK>& x, Pack<T, V>& dy)
+{
+    const long long at = (long long)ch * a.p + t.px;
+    dy = zero_pack<T, V>();
+    if constexpr (CK) {
+        x.e = 1;
+#pragma unroll
+        for (int j = 0; j < V; ++j) x.q.v[j] = 0;
+    } else x.a = zero_pack<T, V>();
+    if (!t.live) return;
+    dy = load_pack<T, V>(static_cast<const T*>(a.dy) + t.n * a.dy_stride + at);
+    if constexpr (CK) {
+        const long long run = t.n * a.c + ch;
+        x.q = load_pack<unsigned char, V>(a.ck.q + run * a.ck.pitch + t.px);
+        x.e = a.ck.steps[run * a.ck.blocks + t.px / kBlock];
+    } else x.a = load_pack<T, V>(static_cast<const T*>(a.x) + t.n * a.x_stride + at);
+}
+
+// FULL as above.  Adds this tile's part of the warp's channel sums to dw and db of lane l for channel l.
+template <class T, int V, int CPT, bool CK, bool FULL>
+__device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, int share, int number, float* red, const float2* wb, float& dw, float& db)
+{
+    const int lane = threadIdx.x & 31, count = FULL ? CPT : t.count;
+    const bool live = FULL || t.live;
+    const unsigned bytes = (unsigned)a.p * sizeof(T);
+    const float inv_c = 1.f / (float)a.c;
+    const long long at = (long long)t.first * a.p + t.px, run = t.n * a.c + t.first;
+    const char* xt = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + t.n * a.x_stride + at);
+    const char* dt = reinterpret_cast<const char*>(static_cast<const T*>(a.dy) + t.n * a.dy_stride + at);
+    const char* qt = reinterpret_cast<const char*>(a.ck.q + run * a.ck.pitch + t.px);
+    const unsigned char* et = a.ck.steps + run * a.ck.blocks + t.px / kBlock;
+    Raw<T, V, CK> x[CPT];
+    Pack<T, V> dy[CPT];
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+        if (!FULL) { dy[i] = zero_pack<T, V>(); x[i].clear(); }
+        if (i < count && live) {
+            dy[i] = load_pack<T, V>(reinterpret_cast<const T*>(plane(dt, bytes, i)));
+            if constexpr (CK) {
+                x[i].q = load_pack<unsigned char, V>(reinterpret_cast<const unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)));
+                x[i].e = et[(unsigned long long)(unsigned)a.ck.blocks * i];
+            } else x[i].a = load_pack<T, V>(reinterpret_cast<const T*>(plane(xt, bytes, i)));
+        }
+    }
+    Vals<V> rstd, shift, s[2] = {all<V>(0.f), all<V>(0.f)};
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        rstd.v[j] = live ? a.rstd[t.row + j] : 0.f;
+        shift.v[j] = live ? -a.mean[t.row + j] * rstd.v[j] : 0.f;
+    }
+    float sums[CPT];
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+        sums[i] = 0.f;
+        if (i >= count) continue;
+        const float w = wb[t.first + i].x;
+        const Vals<V> d = values(dy[i]), dh = mul(d, x[i].hats(rstd, shift));
+        s[0] = fma(d, all<V>(w), s[0]);
+        s[1] = fma(dh, all<V>(w), s[1]);
+        sums[i] = sum_of(dh);
+    }
+    if (a.partials) {
+        dw += across_lanes<CPT>(sums, lane);
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) sums[i] = i < count ? sum_of(values(dy[i])) : 0.f;
+        db += across_lanes<CPT>(sums, lane);
+    }
+    pixel_sum<2, V>(s, share, number, red);
+    if (!a.out) return;
+    const Vals<V> m0 = mul(mul(s[0], all<V>(-inv_c)), rstd), m1 = mul(mul(s[1], all<V>(-inv_c)), rstd);
+    char* out = reinterpret_cast<char*>(static_cast<T*>(a.out) + t.n * a.out_stride + at);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i)
+        if (i < count && live)
+            store_pack<T, V>(reinterpret_cast<T*>(plane(out, bytes, i)),
+                             rounded<T, V>(fma(x[i].hats(rstd, shift), m1, fma(values(dy[i]), mul(rstd, all<V>(wb[t.first + i].x)), m0))));
+}
+
+// Lane l < CPT of a warp keeps the sums of the warp's channel l over all tiles of the block's group.
+template <class T, int V, int CPT, bool CK>
+__global__ void __launch_bounds__(512) norm_bwd_map_kernel(NormArgs a, int share, int per, int tiles)
+{
+    extern __shared__ float smem[];                      // weight and bias, then [2][warps][2][V * 32]
+    previous_launches();
+    next_launch();
+    float2* wb = reinterpret_cast<float2*>(smem);
+    float* red = smem + 2 * a.c;
+    stage_cols(a, wb);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / share, groups = (blockDim.x >> 5) / share;
+    const int half = blockDim.x * V * 2;
+    float dw = 0.f, db = 0.f;
+    int turn = 0;
+    for (long long tile = (long long)blockIdx.x * groups + group; tile < a.n * tiles; tile += (long long)gridDim.x * groups, turn ^= 1) {
+        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, (warp & (share - 1)) * per, per);
+        if (t.count == CPT && t.px - lane * V + 32 * V <= a.p)
+            norm_bwd_tile<T, V, CPT, CK, true>(a, t, share, group + 1, red + turn * half, wb, dw, db);
+        else
+            norm_bwd_tile<T, V, CPT, CK, false>(a, t, share, group + 1, red + turn * half, wb, dw, db);
+    }
+    if (!a.partials) return;
+    __syncthreads();
+    red[threadIdx.x] = dw;
+    red[blockDim.x + threadIdx.x] = db;
+    __syncthreads();
+    const int ch = (warp & (share - 1)) * per + lane;
+    if (group == 0 && lane < per && ch < a.c) {
+        float* set = a.partials + (long long)blockIdx.x * 2 * a.c;
+        for (int k = 0; k < 2; ++k) {
+            float s = 0.f;
+            for (int g = 0; g < groups; ++g) s += red[k * blockDim.x + g * share * 32 + threadIdx.x];
+            set[(long long)k * a.c + ch] = s;
+        }
+    }
+}
+
+// More channels than that: two passes, the sums of a channel grow in the block's own set.
+template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_bwd_long_map_kernel(NormArgs a, int tiles)
+{
+    __shared__ float red[2][512 * V * 2 <= 2048 ? 512 * V * 2 : 2048];
+    previous_launches();
+    next_launch();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const float inv_c = 1.f / (float)a.c;
     float* set = a.partials ? a.partials + (long long)blockIdx.x * 2 * a.c : nullptr;
     int turn = 0;
     for (long long tile = blockIdx.x; tile < a.n * tiles; tile += gridDim.x, turn ^= 1) {
-        const Tile t = tile_of(a, tile, tiles, lp * V, l * V);
-        const T* xt = static_cast<const T*>(a.x) + t.n * a.x_stride + t.px;
-        const T* dyt = static_cast<const T*>(a.dy) + t.n * a.dy_stride + t.px;
-        auto load = [&](int i, Raw<T, V, CK>& x, Pack<T, V>& dy) {
-            const int ch = g + i * groups;
-            const bool there = t.live && ch < a.c;
-            dy = there ? load_pack<T, V>(dyt + (long long)ch * a.p) : zero_pack<T, V>();
-            if constexpr (CK) {
-                const long long run = t.n * a.c + ch;
-                x.e = 0;
-                if (there) {
-                    x.q = load_pack<unsigned char, V>(a.ck.q + run * a.ck.pitch + t.px);
-                    x.e = a.ck.steps[run * a.ck.blocks + t.px / kBlock];
-                } else
-                    for (int j = 0; j < V; ++j) x.q.v[j] = 0;
-            } else x.a = there ? load_pack<T, V>(xt + (long long)ch * a.p) : zero_pack<T, V>();
-        };
-        Raw<T, V, CK> x[R];
-        Pack<T, V> dy[R];
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) load(i, x[i], dy[i]);
-        }
-        float mean[V], rstd[V], s[2][V];
+        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, 0, a.c);
+        Vals<V> rstd, shift, s[2] = {all<V>(0.f), all<V>(0.f)};
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            mean[j] = t.live ? a.mean[t.row + j] : 0.f;
-            rstd[j] = t.live ? a.rstd[t.row + j] : 0.f;
-            s[0][j] = s[1][j] = 0.f;
+            rstd.v[j] = t.live ? a.rstd[t.row + j] : 0.f;
+            shift.v[j] = t.live ? -a.mean[t.row + j] * rstd.v[j] : 0.f;
         }
-        auto sum = [&](const Raw<T, V, CK>& xr, const Pack<T, V>& dr, int i, float& dw_i, float& db_i) {
-            const int ch = g + i * groups;
-            if (ch >= a.c) return;
+        Raw<T, V, CK> x;
+        Pack<T, V> dy;
+        const bool first = tile == blockIdx.x;
+        for (int ch = warp; ch < a.c; ch += warps) {
+            load_map<T, V, CK>(a, t, ch, x, dy);
             const float w = a.weight ? __ldg(a.weight + ch) : 1.f;
-            float xv[V];
-            xr.values(xv);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = to_f(dr.v[j]), hat = (xv[j] - mean[j]) * rstd[j], gr = d * w;
-                s[0][j] += gr;
-                s[1][j] = fmaf(gr, hat, s[1][j]);
-                dw_i = fmaf(d, hat, dw_i);
-                db_i += d;
-            }
-        };
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) sum(x[i], dy[i], i, dw[i], db[i]);
-        } else {
-            for (int i = 0; i < slots; ++i) {
-                float w1 = 0.f, b1 = 0.f;
-                load(i, x[0], dy[0]);
-                sum(x[0], dy[0], i, w1, b1);
-                if (set) {                                   // the channel's sums grow in the block's own set
-                    w1 = lanes_sum(w1, lp); b1 = lanes_sum(b1, lp);
-                    const int ch = g + i * groups;
-                    if (l == 0 && ch < a.c) {
-                        const bool first = tile == blockIdx.x;
-                        set[ch] = w1 + (first ? 0.f : set[ch]);
-                        set[a.c + ch] = b1 + (first ? 0.f : set[a.c + ch]);
-                    }
+            const Vals<V> d = values(dy), dh = mul(d, x.hats(rstd, shift));
+            s[0] = fma(d, all<V>(w), s[0]);
+            s[1] = fma(dh, all<V>(w), s[1]);
+            if (set) {
+                const float w1 = lanes_sum(sum_of(dh)), b1 = lanes_sum(sum_of(d));
+                if (lane == 0) {
+                    set[ch] = w1 + (first ? 0.f : set[ch]);
+                    set[a.c + ch] = b1 + (first ? 0.f : set[a.c + ch]);
                 }
             }
         }
-        pixel_sum<2, V>(s, lp, smem + turn * red);
-        auto finish = [&](const Raw<T, V, CK>& xr, const Pack<T, V>& dr, int i) {
-            const int ch = g + i * groups;
-            if (!t.live || ch >= a.c) return;
-            const float w = a.weight ? __ldg(a.weight + ch) : 1.f;
-            float xv[V];
-            xr.values(xv);
-            Pack<T, V> dx;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float hat = (xv[j] - mean[j]) * rstd[j];
-                dx.v[j] = from_f<T>((fmaf(to_f(dr.v[j]), w, -s[0][j] * inv_c) - hat * (s[1][j] * inv_c)) * rstd[j]);
-            }
-            store_pack<T, V>(static_cast<T*>(a.out) + t.n * a.out_stride + t.px + (long long)ch * a.p, dx);
-        };
+        pixel_sum<2, V>(s, warps, 1, red[turn]);
         if (!a.out) continue;
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) finish(x[i], dy[i], i);
-        } else
-            for (int i = 0; i < slots; ++i) { load(i, x[0], dy[0]); finish(x[0], dy[0], i); }
-    }
-    if (CPT == 0 || !set) return;
-    next_launch();
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const float w1 = lanes_sum(dw[i], lp), b1 = lanes_sum(db[i], lp);
-        const int ch = g + i * groups;
-        if (l == 0 && ch < a.c) { set[ch] = w1; set[a.c + ch] = b1; }
+        const Vals<V> m0 = mul(mul(s[0], all<V>(-inv_c)), rstd), m1 = mul(mul(s[1], all<V>(-inv_c)), rstd);
+        for (int ch = warp; ch < a.c; ch += warps) {
+            load_map<T, V, CK>(a, t, ch, x, dy);
+            const float w = a.weight ? __ldg(a.weight + ch) : 1.f;
+            if (t.live)
+                store_pack<T, V>(static_cast<T*>(a.out) + t.n * a.out_stride + (long long)ch * a.p + t.px,
+                                 rounded<T, V>(fma(x.hats(rstd, shift), m1, fma(mul(values(dy), all<V>(w)), rstd, m0))));
+        }
     }
 }
 
 // ---- sum of the partial sets ------------------------------------------------------------------------------------
-// Columns 0 .. 2 c - 1 of `sets` sets: 32 columns a block, its 8 warps take every eighth set, then one adds the eight sums.
-__global__ void __launch_bounds__(256) norm_reduce_kernel(const float* partials, int sets, int c, float* dweight, float* dbias)
+// Columns 0 .. 2 c - 1 of `sets` sets: 32 columns a block, its 32 warps take every 32nd set, then one adds the 32 sums.
+__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* partials, int sets, int c, float* dweight, float* dbias)
 {
-    __shared__ float part[8][33];
+    __shared__ float part[32][33];
     previous_launches();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long col = (long long)blockIdx.x * 32 + lane, width = 2LL * c;
+    const long long width = 2LL * c, col = (long long)blockIdx.x * 32 + lane;
     float s = 0.f;
     if (col < width)
-        for (int i = warp; i < sets; i += 8) s += partials[i * width + col];
+#pragma unroll 8
+        for (int i = warp; i < sets; i += 32) s += partials[i * width + col];
     part[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && col < width) {
-        s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += part[i][lane];
-        if (col < c) dweight[col] = s; else dbias[col - c] = s;
+    s = lanes_sum(part[lane][warp]);
+    const long long own = (long long)blockIdx.x * 32 + warp;
+    if (lane == 0 && own < width) {
+        if (own < c) dweight[own] = s; else dbias[own - c] = s;
     }
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------
 int pow2_at_least(long long v) { int r = 1; while (r < v) r <<= 1; return r; }
 
-constexpr int kMostSets = 4 * kSms;           // blocks of a backward pass, each with a partial set
+constexpr int kMostSets = 2 * kSms;           // blocks of a backward pass, each with a partial set
+unsigned fewer(long long a, long long b) { return (unsigned)(a < b ? a : b); }
 
-template <class T, int V, int VPT, bool SHIFT, bool CK> int run_fwd_rows(const NormArgs& a, int tpr, LaunchStream ls)
+template <class T, int V, int VPT, int FORM, bool CK, int MOST> int run_fwd_rows(const NormArgs& a, int tpr, LaunchStream ls)
 {
-    const int threads = tpr > kRowThreads ? tpr : kRowThreads, per = threads / tpr;
-    const long long want = (a.rows + per - 1) / per, most = (long long)kSms * (2048 / threads);
-    launch(norm_fwd_rows_kernel<T, V, VPT, SHIFT, CK>, dim3((unsigned)(want < most ? want : most)), dim3(threads), 0, ls, a, tpr);
+    const int threads = tpr > 128 ? tpr : 128, per = threads / tpr;
+    launch(norm_fwd_rows_kernel<T, V, VPT, FORM, CK, MOST>, dim3(fewer((a.rows + per - 1) / per, (long long)kSms * (1024 / threads))), dim3(threads), 0, ls, a, tpr);
     return launched();
 }
-template <class T, int V, bool SHIFT, bool CK> int pick_fwd_rows(const NormArgs& a, LaunchStream ls)
+// 32 values to a thread where the row fills a warp that way, else one vector.
+template <class T, int V, int FORM, bool CK> int pick_fwd_rows(const NormArgs& a, LaunchStream ls)
 {
-    const long long vecs = (a.c + (SHIFT ? V - 1 : 0) + V - 1) / V;
-    const int least = V == 1 ? 32 : 8;
+    const long long vecs = (a.c + (FORM == kShift ? V - 1 : 0) + V - 1) / V;
+    const int least = kBlock / V < 8 ? 8 : kBlock / V;
     auto group = [&](int vpt) { const int t = pow2_at_least((vecs + vpt - 1) / vpt); return t < least ? least : t; };
-    if constexpr (V == 1) {
-        if (vecs <= 4 * 1024) return run_fwd_rows<T, V, 4, SHIFT, CK>(a, group(4), ls);
-        if (vecs <= 16 * 1024) return run_fwd_rows<T, V, 16, SHIFT, CK>(a, group(16), ls);
-    } else {
-        if (vecs <= 512) return run_fwd_rows<T, V, 1, SHIFT, CK>(a, group(1), ls);
-        if (vecs <= 2 * 1024) return run_fwd_rows<T, V, 2, SHIFT, CK>(a, group(2), ls);
-        if (vecs <= 8 * 1024) return run_fwd_rows<T, V, 8, SHIFT, CK>(a, group(8), ls);
-    }
-    launch(norm_fwd_long_rows_kernel<T, CK>, dim3((unsigned)(a.rows < 2 * kSms ? a.rows : 2 * kSms)), dim3(1024), 0, ls, a);
+    constexpr int kWide = V == 1 ? 16 : 32 / V;
+    if (vecs <= 32) return run_fwd_rows<T, V, 1, FORM, CK, 256>(a, group(1), ls);
+    if (vecs <= kWide * 256) return run_fwd_rows<T, V, kWide, FORM, CK, 256>(a, group(kWide), ls);
+    if (vecs <= kWide * 1024) return run_fwd_rows<T, V, kWide, FORM, CK, 1024>(a, group(kWide), ls);
+    launch(norm_fwd_long_rows_kernel<T, CK>, dim3(fewer(a.rows, 2 * kSms)), dim3(1024), 0, ls, a);
     return launched();
 }
 template <class T, bool CK> int fwd_rows(const NormArgs& a, LaunchStream ls)
@@ -645,130 +772,120 @@ template <class T, bool CK> int fwd_rows(const NormArgs& a, LaunchStream ls)
     const bool on_grid = aligned(a.x, 16) && aligned(a.out, 16) && (one || (a.x_stride % V == 0 && a.out_stride % V == 0));
     const bool same = ((reinterpret_cast<uintptr_t>(a.x) ^ reinterpret_cast<uintptr_t>(a.out)) & 15) == 0 &&
                       (one || (a.x_stride - a.out_stride) % V == 0);
-    if (on_grid) return pick_fwd_rows<T, V, false, CK>(a, ls);
+    if (on_grid) return a.c % V == 0 && a.weight && a.bias && a.w_vec ? pick_fwd_rows<T, V, kFast, CK>(a, ls) : pick_fwd_rows<T, V, kEdge, CK>(a, ls);
     if constexpr (!CK)
-        if (same) return pick_fwd_rows<T, V, true, false>(a, ls);
-    return pick_fwd_rows<T, 1, false, CK>(a, ls);
+        if (same) return pick_fwd_rows<T, V, kShift, false>(a, ls);
+    return pick_fwd_rows<T, 1, kEdge, CK>(a, ls);
 }
 
 int sum_sets(const NormArgs& a, int sets, float* dweight, float* dbias, LaunchStream ls)
 {
     if (!a.partials) return launched();
-    launch(norm_reduce_kernel, dim3((unsigned)((2LL * a.c + 31) / 32)), dim3(256), 0, ls, (const float*)a.partials, sets, a.c, dweight, dbias);
+    launch(norm_reduce_kernel, dim3((unsigned)((2LL * a.c + 31) / 32)), dim3(1024), 0, ls, (const float*)a.partials, sets, a.c, dweight, dbias);
     return launched();
 }
 
-template <class T, int V, int VPT, bool CK> int run_bwd_rows(const NormArgs& a, int tpr, float* dweight, float* dbias, LaunchStream ls)
+template <class T, int V, int VPT, bool FAST, bool CK> int run_bwd_rows(const NormArgs& a, int tpr, float* dweight, float* dbias, LaunchStream ls)
 {
-    const int threads = tpr > kRowThreads ? tpr : kRowThreads, per = threads / tpr;
-    const size_t smem = a.partials ? (size_t)threads * VPT * V * 4 : 0;
-    const long long want = (a.rows + per - 1) / per;
-    const long long most = threads <= 256 ? 4 * kSms : threads <= 512 ? 2 * kSms : kSms;
-    const int blocks = (int)(want < most ? want : most);
-    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, CK>, smem)) return FTP_ERR_CUDA;
-    launch(norm_bwd_rows_kernel<T, V, VPT, CK>, dim3(blocks), dim3(threads), smem, ls, a, tpr);
+    const int per = 512 / tpr;
+    const size_t smem = a.partials ? (size_t)512 * VPT * V * 4 : 0;
+    const int blocks = fewer((a.rows + per - 1) / per, kSms);
+    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FAST, CK>, smem)) return FTP_ERR_CUDA;
+    launch(norm_bwd_rows_kernel<T, V, VPT, FAST, CK>, dim3(blocks), dim3(512), smem, ls, a, tpr);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
-template <class T, int V, bool CK> int pick_bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
+// 16 values to a thread; rows of up to 8192 columns.
+template <class T, int V, bool FAST, bool CK> int pick_bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
     const long long vecs = (a.c + V - 1) / V;
-    const int least = V == 1 ? 32 : 8;
+    const int least = kBlock / V < 8 ? 8 : kBlock / V;
     auto group = [&](int vpt) { const int t = pow2_at_least((vecs + vpt - 1) / vpt); return t < least ? least : t; };
-    if constexpr (V == 1) {
-        if (vecs <= 4 * 1024) return run_bwd_rows<T, V, 4, CK>(a, group(4), dweight, dbias, ls);
-        if (vecs <= 16 * 512) return run_bwd_rows<T, V, 16, CK>(a, group(16), dweight, dbias, ls);
-    } else {
-        if (vecs <= 1024) return run_bwd_rows<T, V, 1, CK>(a, group(1), dweight, dbias, ls);
-        if (vecs <= 4 * 512) return run_bwd_rows<T, V, 4, CK>(a, group(4), dweight, dbias, ls);
-    }
-    const int blocks = (int)(a.rows < 2 * kSms ? a.rows : 2 * kSms);
+    constexpr int kWide = 16 / V;
+    if (vecs <= 32) return run_bwd_rows<T, V, 1, FAST, CK>(a, group(1), dweight, dbias, ls);
+    if (vecs <= kWide * 512) return run_bwd_rows<T, V, kWide, FAST, CK>(a, group(kWide), dweight, dbias, ls);
+    const int blocks = fewer(a.rows, 2 * kSms);
     launch(norm_bwd_long_rows_kernel<T, CK>, dim3(blocks), dim3(1024), 0, ls, a);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
 template <class T, bool CK> int bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
+    auto on_grid = [&](const void* p, long long stride, int v) { return !p || (aligned(p, v * sizeof(T)) && (a.rows == 1 || stride % v == 0)); };
+    auto fits = [&](int v) { return on_grid(a.x, a.x_stride, v) && on_grid(a.dy, a.dy_stride, v) && on_grid(a.out, a.out_stride, v); };
     constexpr int V = 16 / sizeof(T);
-    auto on_grid = [&](const void* p, long long stride) { return !p || (aligned(p, 16) && (a.rows == 1 || stride % V == 0)); };
-    if (on_grid(a.x, a.x_stride) && on_grid(a.dy, a.dy_stride) && on_grid(a.out, a.out_stride))
-        return pick_bwd_rows<T, V, CK>(a, dweight, dbias, ls);
-    return pick_bwd_rows<T, 1, CK>(a, dweight, dbias, ls);
+    if (fits(V))
+        return a.c % V == 0 && a.weight && a.w_vec ? pick_bwd_rows<T, V, true, CK>(a, dweight, dbias, ls) : pick_bwd_rows<T, V, false, CK>(a, dweight, dbias, ls);
+    if constexpr (V == 8)
+        if (fits(2)) return pick_bwd_rows<T, 2, false, CK>(a, dweight, dbias, ls);
+    return pick_bwd_rows<T, 1, false, CK>(a, dweight, dbias, ls);
 }
 
-// Tile shape of maps: as many lanes along the pixels as leave a thread at most `most` channels, but tiles of 32 pixels at least.
-struct MapShapeOf { int lp, threads, cpt; };
-MapShapeOf map_shape(int c, int V, int most)
+// Shape of a launch over maps: warps that share a tile's channels, channels of each, warps of a block.
+struct MapShapeOf { int share, per, warps; };
+MapShapeOf map_shape(int c, int most)
 {
-    MapShapeOf m{32, kMapThreads, 0};
-    auto per = [&] { return (c + m.threads / m.lp - 1) / (m.threads / m.lp); };
-    while (per() > 4 && m.lp * V > 32) m.lp >>= 1;
-    if (per() > most) m.threads = 512;
-    m.cpt = per();
+    MapShapeOf m{};
+    m.share = pow2_at_least((c + most - 1) / most);
+    m.per = (c + m.share - 1) / m.share;
+    m.warps = m.share > 4 ? m.share : 4;
     return m;
 }
 
 template <class T, int V, bool CK> int fwd_map(const NormArgs& a, LaunchStream ls)
 {
-    const MapShapeOf m = map_shape(a.c, V, 16);
-    const long long tiles = (a.p + m.lp * V - 1) / (m.lp * V), all = a.n * tiles;
-    const size_t smem = 2 * (size_t)(m.threads / 32) * m.lp * V * 4;
-    auto go = [&](auto kernel, int per_sm) {
-        const long long most = (long long)kSms * per_sm;
-        if (!allow_smem(kernel, smem)) return (int)FTP_ERR_CUDA;
-        launch(kernel, dim3((unsigned)(all < most ? all : most)), dim3(m.threads), smem, ls, a, m.lp, (int)tiles);
+    const long long tiles = (a.p + 32 * V - 1) / (32 * V), all = a.n * tiles;
+    if (a.c > 1024) {
+        launch(norm_fwd_long_map_kernel<T, V, CK>, dim3(fewer(all, 4 * kSms)), dim3(512), 0, ls, a, (int)tiles);
+        return launched();
+    }
+    const MapShapeOf m = map_shape(a.c, 32);
+    const size_t smem = (size_t)a.c * 8 + 2 * (size_t)m.warps * 32 * V * 4;
+    const long long blocks = (all + m.warps / m.share - 1) / (m.warps / m.share);
+    auto go = [&](auto kernel) {
+        launch(kernel, dim3(fewer(blocks, (long long)kSms * (32 / m.warps))), dim3(m.warps * 32), smem, ls, a, m.share, m.per, (int)tiles);
         return launched();
     };
-    if (m.cpt <= 1) return go(norm_fwd_map_kernel<T, V, 1, CK>, 8);
-    if (m.cpt <= 4) return go(norm_fwd_map_kernel<T, V, 4, CK>, 6);
-    if (m.cpt <= 16) return go(norm_fwd_map_kernel<T, V, 16, CK>, 2);
-    return go(norm_fwd_map_kernel<T, V, 0, CK>, 4);
+    if (m.per <= 8) return go(norm_fwd_map_kernel<T, V, 8, CK, 256>);
+    return m.warps <= 8 ? go(norm_fwd_map_kernel<T, V, 32, CK, 256>) : go(norm_fwd_map_kernel<T, V, 32, CK, 1024>);
 }
 template <class T, int V, bool CK> int bwd_map(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
-    const MapShapeOf m = map_shape(a.c, V, 8);
-    const long long tiles = (a.p + m.lp * V - 1) / (m.lp * V), all = a.n * tiles;
-    const size_t smem = 4 * (size_t)(m.threads / 32) * m.lp * V * 4;
-    auto go = [&](auto kernel, int per_sm) {
-        const long long most = (long long)kSms * per_sm;
-        const int blocks = (int)(all < most ? all : most);
-        if (!allow_smem(kernel, smem)) return (int)FTP_ERR_CUDA;
-        launch(kernel, dim3(blocks), dim3(m.threads), smem, ls, a, m.lp, (int)tiles);
+    const long long tiles = (a.p + 32 * V - 1) / (32 * V), all = a.n * tiles;
+    if (a.c > 512) {
+        const int blocks = fewer(all, kMostSets);
+        launch(norm_bwd_long_map_kernel<T, V, CK>, dim3(blocks), dim3(512 / V), 0, ls, a, (int)tiles);
+        return sum_sets(a, blocks, dweight, dbias, ls);
+    }
+    MapShapeOf m = map_shape(a.c, a.c <= 256 ? 16 : 32);
+    m.warps = m.share > 8 ? m.share : 8;
+    const size_t smem = (size_t)a.c * 8 + 4 * (size_t)m.warps * 32 * V * 4;
+    const int blocks = fewer((all + m.warps / m.share - 1) / (m.warps / m.share), (long long)kSms * (16 / m.warps));
+    auto go = [&](auto kernel) {
+        launch(kernel, dim3(blocks), dim3(m.warps * 32), smem, ls, a, m.share, m.per, (int)tiles);
         return sum_sets(a, blocks, dweight, dbias, ls);
     };
-    if (m.cpt <= 1) return go(norm_bwd_map_kernel<T, V, 1, CK>, 4);
-    if (m.cpt <= 4) return go(norm_bwd_map_kernel<T, V, 4, CK>, 4);
-    if (m.cpt <= 8) return go(norm_bwd_map_kernel<T, V, 8, CK>, 2);
-    return go(norm_bwd_map_kernel<T, V, 0, CK>, 3);
+    return m.per <= 8 ? go(norm_bwd_map_kernel<T, V, 8, CK>) : m.per <= 16 ? go(norm_bwd_map_kernel<T, V, 16, CK>) : go(norm_bwd_map_kernel<T, V, 32, CK>);
 }
 
-// The widest vector of pixels that divides a plane and lies on its own grid in every array.
-template <class T> int map_vector(const NormArgs& a, int most)
+// Whether arrays can be read as pairs of 16-bit pixels.
+template <class T> bool map_pairs(const NormArgs& a)
 {
-    auto fits = [&](const void* p, long long stride, int v) { return !p || (aligned(p, v * sizeof(T)) && (a.n == 1 || stride % v == 0)); };
-    for (int v = most; v > 1; v = v == 8 ? 2 : 1)
-        if (a.p % v == 0 && fits(a.x, a.x_stride, v) && fits(a.dy, a.dy_stride, v) && fits(a.out, a.out_stride, v)) return v;
-    return 1;
+    auto fits = [&](const void* p, long long stride) { return !p || (aligned(p, 4) && (a.n == 1 || stride % 2 == 0)); };
+    return a.p % 2 == 0 && fits(a.x, a.x_stride) && fits(a.dy, a.dy_stride) && fits(a.out, a.out_stride);
 }
 
 template <class T, bool CK> int forward(const NormArgs& a, LaunchStream ls)
 {
     if (a.p == 1) return fwd_rows<T, CK>(a, ls);
-    if constexpr (sizeof(T) == 4)
-        return map_vector<T>(a, 4) == 4 ? fwd_map<T, 4, CK>(a, ls) : fwd_map<T, 1, CK>(a, ls);
-    else {
-        const int v = map_vector<T>(a, 8);
-        return v == 8 ? fwd_map<T, 8, CK>(a, ls) : v == 2 ? fwd_map<T, 2, CK>(a, ls) : fwd_map<T, 1, CK>(a, ls);
-    }
+    if constexpr (sizeof(T) == 2)
+        if (map_pairs<T>(a)) return fwd_map<T, 2, CK>(a, ls);
+    return fwd_map<T, 1, CK>(a, ls);
 }
 template <class T, bool CK> int backward(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
     if (a.p == 1) return bwd_rows<T, CK>(a, dweight, dbias, ls);
-    if constexpr (sizeof(T) == 4)
-        return map_vector<T>(a, 4) == 4 ? bwd_map<T, 4, CK>(a, dweight, dbias, ls) : bwd_map<T, 1, CK>(a, dweight, dbias, ls);
-    else {
-        const int v = map_vector<T>(a, 8);
-        return v == 8 ? bwd_map<T, 8, CK>(a, dweight, dbias, ls)
-             : v == 2 ? bwd_map<T, 2, CK>(a, dweight, dbias, ls) : bwd_map<T, 1, CK>(a, dweight, dbias, ls);
-    }
+    if constexpr (sizeof(T) == 2)
+        if (map_pairs<T>(a)) return bwd_map<T, 2, CK>(a, dweight, dbias, ls);
+    return bwd_map<T, 1, CK>(a, dweight, dbias, ls);
 }
 template <class T> int forward(const NormArgs& a, bool ck, LaunchStream ls) { return ck ? forward<T, true>(a, ls) : forward<T, false>(a, ls); }
 template <class T> int backward(const NormArgs& a, bool ck, float* dw, float* db, LaunchStream ls)
