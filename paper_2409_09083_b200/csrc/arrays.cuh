@@ -147,13 +147,15 @@ template <int V> __device__ __forceinline__ Vals<V> mul(const Vals<V>& a, const 
     }
     return r;
 }
-template <int V> __device__ __forceinline__ float sum_of(Vals<V> a)
+template <int V> __device__ __forceinline__ float sum_of(const Vals<V>& a)
 {
+    if constexpr (V >= 4) {
+        Vals<V / 2> lo, hi;
 #pragma unroll
-    for (int h = V / 2; h >= 1; h >>= 1)
-#pragma unroll
-        for (int j = 0; j < h; ++j) a.v[j] += a.v[j + h];
-    return a.v[0];
+        for (int j = 0; j < V / 2; ++j) { lo.v[j] = a.v[j]; hi.v[j] = a.v[j + V / 2]; }
+        return sum_of(add(lo, hi));
+    } else if constexpr (V == 2) return a.v[0] + a.v[1];
+    else return a.v[0];
 }
 
 template <int V> __device__ __forceinline__ Vals<V> values(const Pack<float, V>& p)
@@ -257,36 +259,24 @@ template <class T> __device__ __forceinline__ bool special(float largest)
     return !(largest <= last);
 }
 
-// The steps of V values whose block is spread over 32 / V neighbouring lanes (all lanes of the warp take part), and its exponent.
-// Adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it in the low byte.
-template <class T, int V> __device__ __forceinline__ Pack<unsigned char, V> to_steps(const Vals<V>& x, unsigned& e)
+// Largest magnitude of a block that is spread, V values each, over 32 / V neighbouring lanes (all lanes of the warp take part); NaN if
+// there is one among them.
+template <int V> __device__ __forceinline__ float largest(const Vals<V>& x, unsigned lanes = 0xffffffffu)
 {
-    float big = 0.f;
+    float big = fabsf(x.v[0]);
 #pragma unroll
-    for (int j = 0; j < V; ++j) big = max_nan(big, fabsf(x.v[j]));
-    if constexpr (V == 1) big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));     // (a NaN's bits are above all)
-    else {
+    for (int j = 1; j < V; ++j) big = max_nan(big, fabsf(x.v[j]));
+    if constexpr (V == 1) return __uint_as_float(__reduce_max_sync(lanes, __float_as_uint(big)));     // (a NaN's bits are above all)
 #pragma unroll
-        for (int d = kBlock / V / 2; d >= 1; d >>= 1) big = max_nan(big, __shfl_xor_sync(0xffffffffu, big, d));
-    }
+    for (int d = kBlock / V / 2; d >= 1; d >>= 1) big = max_nan(big, __shfl_xor_sync(lanes, big, d));
+    return big;
+}
+
+// The steps of V values of a block that is not special().  Adding 1.5 * 2^23 rounds to the nearest integer, ties to even, and leaves it
+// in the low byte.
+template <int V> __device__ __forceinline__ Pack<unsigned char, V> to_steps(const Vals<V>& x, unsigned e)
+{
     Pack<unsigned char, V> q;
-    if (special<T>(big)) {
-        // every lane of the block is here: largest finite magnitude, then each value by itself
-        float finite = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) finite = fabsf(x.v[j]) < INFINITY ? fmaxf(finite, fabsf(x.v[j])) : finite;
-        const unsigned lanes = V == 1 ? 0xffffffffu : ((1u << (kBlock / V % 32)) - 1u) << (threadIdx.x & 31 & ~(kBlock / V - 1));
-        finite = __uint_as_float(__reduce_max_sync(lanes, __float_as_uint(finite)));
-        e = step_exponent(finite);
-        const float inverse = inverse_step(e), most = special<T>(finite) ? 63.f : 127.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float s = fminf(fmaxf(x.v[j] * inverse, -most), most) + 12582912.f;
-            q.v[j] = fabsf(x.v[j]) < INFINITY ? (unsigned char)__float_as_uint(s) : (unsigned char)0x80u;
-        }
-        return q;
-    }
-    e = step_exponent(big);
     const Vals<V> s = fma(x, all<V>(inverse_step(e)), all<V>(12582912.f));
     if constexpr (V % 4 == 0) {
 #pragma unroll
@@ -299,6 +289,26 @@ template <class T, int V> __device__ __forceinline__ Pack<unsigned char, V> to_s
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) q.v[j] = (unsigned char)__float_as_uint(s.v[j]);
+    }
+    return q;
+}
+
+// The same for a special block, by the lanes that hold it: largest finite magnitude, then each value by itself.
+template <class T, int V> __device__ __noinline__ Pack<unsigned char, V> to_steps_special(const Vals<V> x, unsigned& e)
+{
+    constexpr int kLanes = kBlock / V;
+    const unsigned lanes = kLanes == 32 ? 0xffffffffu : ((1u << (kLanes % 32)) - 1u) << (threadIdx.x & 31 & ~(kLanes - 1));
+    Vals<V> finite;
+#pragma unroll
+    for (int j = 0; j < V; ++j) finite.v[j] = fabsf(x.v[j]) < INFINITY ? x.v[j] : 0.f;
+    const float big = largest(finite, lanes);
+    e = step_exponent(big);
+    const float inverse = inverse_step(e), most = special<T>(big) ? 63.f : 127.f;
+    Pack<unsigned char, V> q;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const float s = fminf(fmaxf(finite.v[j] * inverse, -most), most) + 12582912.f;
+        q.v[j] = fabsf(x.v[j]) < INFINITY ? (unsigned char)__float_as_uint(s) : (unsigned char)0x80u;
     }
     return q;
 }
@@ -330,7 +340,8 @@ template <int V> __device__ __forceinline__ Vals<V> steps_of(const Pack<unsigned
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) r.v[j] = q.v[j] == 0x80u ? nan_f() : (float)(signed char)q.v[j];
+        for (int j = 0; j < V; ++j)
+            r.v[j] = q.v[j] == 0x80u ? nan_f() : __uint_as_float((unsigned)(q.v[j] ^ 0x80u) | 0x4b000000u) - 8388736.f;
     }
     return r;
 }
@@ -386,6 +397,18 @@ inline CkptView ckpt_view(const ftp_dims* d, const void* ckpt)
 template <class K> inline bool allow_smem(K kernel, size_t bytes)
 {
     return bytes <= 48 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+}
+// Blocks of a kernel that an SM holds at once, from its registers (asked for once) and the launch's shared memory: persistent grids are
+// that many an SM, or their last blocks would wait for the first to end.
+template <auto K> inline int resident(int threads, size_t smem)
+{
+    static const cudaFuncAttributes at = [] { cudaFuncAttributes a{}; if (cudaFuncGetAttributes(&a, K) != cudaSuccess) a.numRegs = 255; return a; }();
+    const int regs = (at.numRegs + 7) / 8 * 8;
+    const size_t shared = smem + at.sharedSizeBytes + 1024;
+    const int by_regs = 65536 / (regs * threads), by_smem = (int)(233472 / shared), by_threads = 2048 / threads;
+    int n = by_regs < by_smem ? by_regs : by_smem;
+    n = n < by_threads ? n : by_threads;
+    return n < 1 ? 1 : n > 32 ? 32 : n;
 }
 inline int launched() { return cudaGetLastError() == cudaSuccess ? FTP_OK : FTP_ERR_CUDA; }
 

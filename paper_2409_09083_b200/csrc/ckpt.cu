@@ -47,11 +47,28 @@ template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads)
                 const long long e = first + i * 32 * V;
                 raw[i] = e < a.len ? load_part<T, V>(x, e, 0, a.len) : zero_pack<T, V>();
             }
+            // every block as if it held finite values only, then the others again
+            bool any = false;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const long long e = first + i * 32 * V;
+                const Vals<V> v = values(raw[i]);
+                const float big = largest(v);
+                any |= special<T>(big);
+                const unsigned ex = step_exponent(big);
+                if (e < a.ck.pitch) {
+                    store_pack<unsigned char, V>(q + e, to_steps(v, ex));
+                    if (e % kBlock == 0) steps[e / kBlock] = (unsigned char)ex;
+                }
+            }
+            if (!__any_sync(0xffffffffu, any)) continue;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const long long e = first + i * 32 * V;
+                const Vals<V> v = values(raw[i]);
+                if (!special<T>(largest(v))) continue;
                 unsigned ex;
-                const Pack<unsigned char, V> b = to_steps<T, V>(values(raw[i]), ex);
+                const Pack<unsigned char, V> b = to_steps_special<T, V>(v, ex);
                 if (e < a.ck.pitch) {
                     store_pack<unsigned char, V>(q + e, b);
                     if (e % kBlock == 0) steps[e / kBlock] = (unsigned char)ex;

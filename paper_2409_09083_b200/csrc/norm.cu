@@ -32,9 +32,10 @@ struct NormArgs {
     int w_vec;                   // weight and bias are 16-byte aligned
 };
 
-// Adds over the `tpr` threads of a group; tpr a power of two, groups within a warp or a whole number of warps with barrier `number`.
-// `red`: K floats a warp, not read or written by anyone else until the group has passed another barrier.
-template <int K> __device__ __forceinline__ void group_sum(float (&v)[K], int tpr, int number, float* red)
+// Adds over the `tpr` threads of a group; tpr a power of two, groups within a warp, or the block (number 0), or a whole number of warps with a
+// barrier `number` of their own (an SM has 64 barriers and a kernel that names them at run time takes 16 a block: for kernels of one
+// block an SM).  `red`: K floats a warp, not read or written by anyone else until the group has passed another barrier.
+template <int K, bool NAMED = false> __device__ __forceinline__ void group_sum(float (&v)[K], int tpr, int number, float* red)
 {
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = lanes_sum(v[k], tpr);
@@ -44,7 +45,8 @@ template <int K> __device__ __forceinline__ void group_sum(float (&v)[K], int tp
 #pragma unroll
         for (int k = 0; k < K; ++k) red[warp * K + k] = v[k];
     }
-    group_barrier(number, tpr);
+    if constexpr (NAMED) group_barrier(number, tpr);
+    else __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = 0.f;
 #pragma unroll 4
@@ -127,7 +129,7 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_rows_kerne
             for (int j = 0; j < V; ++j) x.v[i * V + j] = v.v[j];
         }
         float s[1] = {sum_of(x)};
-        group_sum<1>(s, tpr, group + 1, red[0]);
+        group_sum<1>(s, tpr, 0, red[0]);
         const float mean = a.c == 1 ? s[0] : s[0] * inv_c;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -146,21 +148,24 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_rows_kerne
             for (int j = 0; j < V; ++j) x.v[i * V + j] = v.v[j];
         }
         s[0] = sum_of(mul(x, x));
-        group_sum<1>(s, tpr, group + 1, red[1]);
+        group_sum<1>(s, tpr, 0, red[1]);
         const float rstd = 1.f / sqrtf(s[0] * inv_c + a.eps);
         if (live && t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
         T* yr = static_cast<T*>(a.out) + row * a.out_stride - o;
+        bool any = false;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            if (CK) {
-                unsigned ex;
-                const Pack<unsigned char, V> st = to_steps<T, V>(values(raw[i]), ex);
+            if (CK) {                                           // as if all values were finite
+                const Vals<V> v = values(raw[i]);
+                const float big = largest(v);
+                any |= special<T>(big);
+                const unsigned ex = step_exponent(big);
                 if (live && e < a.ck.pitch) {
-                    store_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e, st);
+                    store_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e, to_steps(v, ex));
                     if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
                 }
             }
@@ -173,6 +178,20 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_rows_kerne
                 const Pack<T, V> y = rounded<T, V>(fma(mul(v, all<V>(rstd)), w, b));
                 if (kWhole) store_pack<T, V>(yr + e, y);
                 else store_part<T, V>(yr, e, o, hi, y);
+            }
+        }
+        if (CK && __any_sync(0xffffffffu, any)) {               // the blocks with others once more
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int e = (i * tpr + t) * V;
+                const Vals<V> v = values(raw[i]);
+                if (!special<T>(largest(v))) continue;
+                unsigned ex;
+                const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
+                if (live && e < a.ck.pitch) {
+                    store_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e, st);
+                    if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
+                }
             }
         }
     }
@@ -188,10 +207,10 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
         T* yr = static_cast<T*>(a.out) + row * a.out_stride;
         float s[1] = {0.f}, q[1] = {0.f};
         for (int e = threadIdx.x; e < a.c; e += 1024) s[0] += to_f(xr[e]);
-        group_sum<1>(s, 1024, 1, red[0]);
+        group_sum<1>(s, 1024, 0, red[0]);
         const float mean = s[0] / (float)a.c;
         for (int e = threadIdx.x; e < a.c; e += 1024) { const float d = to_f(xr[e]) - mean; q[0] = fmaf(d, d, q[0]); }
-        group_sum<1>(q, 1024, 1, red[1]);
+        group_sum<1>(q, 1024, 0, red[1]);
         const float rstd = 1.f / sqrtf(q[0] / (float)a.c + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -202,8 +221,9 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
             Pack<T, 1> v = zero_pack<T, 1>();
             if (e < a.c) v.v[0] = xr[e];
             if (CK) {
-                unsigned ex;
-                const Pack<unsigned char, 1> st = to_steps<T, 1>(values(v), ex);
+                const float big = largest(values(v));
+                unsigned ex = step_exponent(big);
+                const Pack<unsigned char, 1> st = special<T>(big) ? to_steps_special<T, 1>(values(v), ex) : to_steps(values(v), ex);
                 a.ck.q[row * a.ck.pitch + e] = st.v[0];
                 if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
             }
@@ -222,29 +242,30 @@ template <class T, int V, int VPT, bool CK> struct RowIn {
     Pack<T, V> dy[VPT];
     float mean, rstd;
 };
+// Where a thread's first vector of a row lies; the others follow at multiples of tpr vectors.
+template <class T> struct RowAt {
+    const T *x, *dy;
+    T* out;
+    const unsigned char *q, *e;
+    const float *mean, *rstd;
+};
 template <class T, int V, int VPT, bool FAST, bool CK>
-__device__ __forceinline__ void load_row(const NormArgs& a, long long row, int tpr, int t, RowIn<T, V, VPT, CK>& in)
+__device__ __forceinline__ void load_row(const RowAt<T>& at, bool live, int c, int tpr, int t, RowIn<T, V, VPT, CK>& in)
 {
     constexpr bool kWhole = FAST || V == 1;
-    const bool live = row < a.rows;
-    const int c = live ? a.c : 0;
-    const T* dyr = static_cast<const T*>(a.dy) + row * a.dy_stride;
-    const T* xr = static_cast<const T*>(a.x) + row * a.x_stride;
-    const unsigned char* qr = a.ck.q + row * a.ck.pitch;
-    const unsigned char* er = a.ck.steps + row * a.ck.blocks;
     in.mean = in.rstd = 0.f;
-    if (live) { in.mean = a.mean[row]; in.rstd = a.rstd[row]; }
+    if (live) { in.mean = *at.mean; in.rstd = *at.rstd; }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        const int e = (i * tpr + t) * V;
+        const int skip = i * tpr * V, e = skip + t * V;
         in.dy[i] = zero_pack<T, V>();
         in.x[i].clear();
-        if (e < c) {
-            in.dy[i] = kWhole ? load_pack<T, V>(dyr + e) : load_part<T, V>(dyr, e, 0, c);
+        if (live && e < c) {
+            in.dy[i] = kWhole ? load_pack<T, V>(at.dy + skip) : load_part<T, V>(at.dy - t * V, e, 0, c);
             if constexpr (CK) {
-                in.x[i].q = load_pack<unsigned char, V>(qr + e);
-                in.x[i].e = er[e / kBlock];
-            } else in.x[i].a = kWhole ? load_pack<T, V>(xr + e) : load_part<T, V>(xr, e, 0, c);
+                in.x[i].q = load_pack<unsigned char, V>(at.q + skip);
+                in.x[i].e = at.e[skip / kBlock];
+            } else in.x[i].a = kWhole ? load_pack<T, V>(at.x + skip) : load_part<T, V>(at.x - t * V, e, 0, c);
         }
     }
 }
@@ -263,45 +284,59 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
     Vals<E> dw = all<E>(0.f), db = all<E>(0.f);
     const long long step = (long long)gridDim.x * per;
     long long row = (long long)blockIdx.x * per + group;
+    RowAt<T> at;
+    at.x = static_cast<const T*>(a.x) + row * a.x_stride + t * V;
+    at.dy = static_cast<const T*>(a.dy) + row * a.dy_stride + t * V;
+    at.out = static_cast<T*>(a.out) + row * a.out_stride + t * V;
+    at.q = a.ck.q + row * a.ck.pitch + t * V;
+    at.e = a.ck.steps + row * a.ck.blocks + t * V / kBlock;
+    at.mean = a.mean + row;
+    at.rstd = a.rstd + row;
     RowIn<T, V, VPT, CK> next;
-    load_row<T, V, VPT, FAST, CK>(a, row, tpr, t, next);
+    load_row<T, V, VPT, FAST, CK>(at, row < a.rows, a.c, tpr, t, next);
     int turn = 0;
     // (groups narrower than a warp stay together: a warp goes on until none of its rows is left)
     for (long long first = (long long)blockIdx.x * per + (tpr < 32 ? (threadIdx.x & ~31) / tpr : group); first < a.rows; first += step, turn ^= 1) {
         const float rstd = next.rstd, shift = -next.mean * next.rstd;
-        Vals<E> d, g, hat;
+        Vals<E> d, hat;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const Vals<V> di = values(next.dy[i]), hi = next.x[i].hats(rstd, shift);
+#pragma unroll
+            for (int j = 0; j < V; ++j) { d.v[i * V + j] = di.v[j]; hat.v[i * V + j] = hi.v[j]; }
+        }
+        const bool live = row < a.rows;
+        row += step;
+        at.x += step * a.x_stride; at.dy += step * a.dy_stride;
+        at.q += step * a.ck.pitch; at.e += step * a.ck.blocks;
+        at.mean += step; at.rstd += step;
+        load_row<T, V, VPT, FAST, CK>(at, row < a.rows, a.c, tpr, t, next);
+        dw = fma(d, hat, dw);
+        db = add(db, d);
+        Vals<E> w = all<E>(0.f);                       // (from L1: 16 registers more would spill)
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            const Vals<V> di = values(next.dy[i]), hi = next.x[i].hats(rstd, shift);
-            Vals<V> w = all<V>(0.f);
-            if (e < a.c) load_cols<FAST, V>(a.weight, e, a.c, 1.f, w.v);
-            const Vals<V> gi = mul(di, w);
-#pragma unroll
-            for (int j = 0; j < V; ++j) { d.v[i * V + j] = di.v[j]; g.v[i * V + j] = gi.v[j]; hat.v[i * V + j] = hi.v[j]; }
+            if (e < a.c) load_cols<FAST, V>(a.weight, e, a.c, 1.f, w.v + i * V);
         }
-        const long long here = row;
-        row += step;
-        load_row<T, V, VPT, FAST, CK>(a, row, tpr, t, next);
-        dw = fma(d, hat, dw);
-        db = add(db, d);
+        const Vals<E> g = mul(d, w);
         float s[2] = {sum_of(g), sum_of(mul(g, hat))};
-        group_sum<2>(s, tpr, group + 1, red[turn]);
-        if (a.out && here < a.rows) {
+        group_sum<2, true>(s, tpr, group + 1, red[turn]);
+        if (a.out && live) {
             const Vals<E> dx = fma(hat, all<E>(-s[1] * inv_c * rstd), fma(g, all<E>(rstd), all<E>(-s[0] * inv_c * rstd)));
-            T* out = static_cast<T*>(a.out) + here * a.out_stride;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int e = (i * tpr + t) * V;
+                const int skip = i * tpr * V, e = skip + t * V;
                 Vals<V> v;
 #pragma unroll
                 for (int j = 0; j < V; ++j) v.v[j] = dx.v[i * V + j];
                 if (e < a.c) {
-                    if (kWhole) store_pack<T, V>(out + e, rounded<T, V>(v));
-                    else store_part<T, V>(out, e, 0, a.c, rounded<T, V>(v));
+                    if (kWhole) store_pack<T, V>(at.out + skip, rounded<T, V>(v));
+                    else store_part<T, V>(at.out - t * V, e, 0, a.c, rounded<T, V>(v));
                 }
             }
         }
+        at.out += step * a.out_stride;
     }
     if (!a.partials) return;
     const int width = tpr * E;
@@ -348,7 +383,7 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_lon
             s[0] += g;
             s[1] = fmaf(g, hat_of(e), s[1]);
         }
-        group_sum<2>(s, 1024, 1, red[turn]);
+        group_sum<2>(s, 1024, 0, red[turn]);
         const float m0 = s[0] * inv_c, m1 = s[1] * inv_c;
         const bool first = row == blockIdx.x;
         for (int e = threadIdx.x; e < a.c; e += 1024) {
@@ -365,9 +400,9 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_lon
 }
 
 // ---- maps -------------------------------------------------------------------------------------------------------
-// A tile is 32 V pixels of one sample with all channels: a lane has V pixels (4 bytes of them, or one value), and the `share` warps of
-// a group split the channels, `per` <= CPT to a warp, which stay in registers.  A block holds one or more groups.  With up to 32 channels
-// a warp works alone, without a barrier.
+// A tile is 32 V pixels of one sample with all channels: a lane has V pixels (4 bytes of them, or one value), and `share` warps split
+// the channels, `per` <= CPT to a warp, which stay in registers.  If share > 1 these are the block; if one warp holds all channels, the
+// warps of a block take a tile each and need no barrier.
 struct Tile { long long n, row; int px, first, count; bool live; };
 
 __device__ __forceinline__ Tile tile_of(const NormArgs& a, long long tile, int tiles, int pixels, int at, int first, int per)
@@ -382,16 +417,16 @@ __device__ __forceinline__ Tile tile_of(const NormArgs& a, long long tile, int t
     return t;
 }
 
-// Adds K values of each pixel over the `share` warps of a group, in their order.
-template <int K, int V> __device__ __forceinline__ void pixel_sum(Vals<V> (&v)[K], int share, int number, float* red)
+// Adds K values of each pixel over the `share` warps of the block, in their order (1: the warp's own).
+template <int K, int V> __device__ __forceinline__ void pixel_sum(Vals<V> (&v)[K], int share, float* red)
 {
     if (share == 1) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp & ~(share - 1);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) red[((warp * K + k) * V + j) * 32 + lane] = v[k].v[j];
-    group_barrier(number, share * 32);
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = all<V>(0.f);
 #pragma unroll 4
@@ -399,7 +434,7 @@ template <int K, int V> __device__ __forceinline__ void pixel_sum(Vals<V> (&v)[K
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[k].v[j] += red[(((first + w) * K + k) * V + j) * 32 + lane];
+            for (int j = 0; j < V; ++j) v[k].v[j] += red[((w * K + k) * V + j) * 32 + lane];
 }
 
 // Bytes from a place of channel 0 to the same place of channel i: one wide multiply-add.
@@ -415,7 +450,7 @@ __device__ __forceinline__ void stage_cols(const NormArgs& a, float2* wb)
 
 // FULL: all CPT channels and all pixels of the tile are there, which spares four tests for every value.
 template <class T, int V, int CPT, bool CK, bool FULL>
-__device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, int share, int number, float* red, int half, const float2* wb)
+__device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, int share, float* red, int half, const float2* wb)
 {
     const int count = FULL ? CPT : t.count;
     const bool live = FULL || t.live;
@@ -432,13 +467,13 @@ __device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, 
     Vals<V> s[1] = {all<V>(0.f)};
 #pragma unroll
     for (int i = 0; i < CPT; ++i) s[0] = add(s[0], values(raw[i]));
-    pixel_sum<1, V>(s, share, number, red);
+    pixel_sum<1, V>(s, share, red);
     const Vals<V> mean = a.c == 1 ? s[0] : mul(s[0], all<V>(inv_c)), minus = mul(mean, all<V>(-1.f));
     s[0] = all<V>(0.f);
 #pragma unroll
     for (int i = 0; i < CPT; ++i)
         if (i < count) { const Vals<V> d = add(values(raw[i]), minus); s[0] = fma(d, d, s[0]); }
-    pixel_sum<1, V>(s, share, number, red + half);
+    pixel_sum<1, V>(s, share, red + half);
     Vals<V> rstd;
 #pragma unroll
     for (int j = 0; j < V; ++j) rstd.v[j] = 1.f / sqrtf(s[0].v[j] * inv_c + a.eps);
@@ -452,14 +487,17 @@ __device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, 
     const long long run = t.n * a.c + t.first;
     char* qt = reinterpret_cast<char*>(a.ck.q + run * a.ck.pitch + t.px);
     unsigned char* et = a.ck.steps + run * a.ck.blocks + t.px / kBlock;
+    bool any = false;
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
         if (i >= count) continue;
-        if (CK) {
-            unsigned ex;
-            const Pack<unsigned char, V> st = to_steps<T, V>(values(raw[i]), ex);
+        if (CK) {                                               // as if all values were finite
+            const Vals<V> v = values(raw[i]);
+            const float big = largest(v);
+            any |= special<T>(big);
+            const unsigned ex = step_exponent(big);
             if (FULL || t.px < a.ck.pitch) {
-                store_pack<unsigned char, V>(reinterpret_cast<unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)), st);
+                store_pack<unsigned char, V>(reinterpret_cast<unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)), to_steps(v, ex));
                 if (t.px % kBlock == 0) et[(unsigned long long)(unsigned)a.ck.blocks * i] = (unsigned char)ex;
             }
         }
@@ -467,6 +505,20 @@ __device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, 
             const float2 c = wb[t.first + i];
             store_pack<T, V>(reinterpret_cast<T*>(plane(yt, bytes, i)),
                              rounded<T, V>(fma(add(values(raw[i]), minus), mul(rstd, all<V>(c.x)), all<V>(c.y))));
+        }
+    }
+    if (CK && __any_sync(0xffffffffu, any)) {                   // the blocks with others once more
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) {
+            if (i >= count) continue;
+            const Vals<V> v = values(raw[i]);
+            if (!special<T>(largest(v))) continue;
+            unsigned ex;
+            const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
+            if (FULL || t.px < a.ck.pitch) {
+                store_pack<unsigned char, V>(reinterpret_cast<unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)), st);
+                if (t.px % kBlock == 0) et[(unsigned long long)(unsigned)a.ck.blocks * i] = (unsigned char)ex;
+            }
         }
     }
 }
@@ -482,8 +534,8 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_map_kernel
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / share, groups = (blockDim.x >> 5) / share;
     for (long long tile = (long long)blockIdx.x * groups + group; tile < a.n * tiles; tile += (long long)gridDim.x * groups) {
         const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, (warp & (share - 1)) * per, per);
-        if (t.count == CPT && t.px - lane * V + 32 * V <= a.p) norm_fwd_tile<T, V, CPT, CK, true>(a, t, share, group + 1, red, blockDim.x * V, wb);
-        else norm_fwd_tile<T, V, CPT, CK, false>(a, t, share, group + 1, red, blockDim.x * V, wb);
+        if (t.count == CPT && t.px - lane * V + 32 * V <= a.p) norm_fwd_tile<T, V, CPT, CK, true>(a, t, share, red, blockDim.x * V, wb);
+        else norm_fwd_tile<T, V, CPT, CK, false>(a, t, share, red, blockDim.x * V, wb);
     }
 }
 
@@ -500,14 +552,14 @@ template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_f
         auto load = [&](int ch) { return t.live ? values(load_pack<T, V>(xt + (long long)ch * a.p)) : all<V>(0.f); };
         Vals<V> s[1] = {all<V>(0.f)};
         for (int ch = warp; ch < a.c; ch += warps) s[0] = add(s[0], load(ch));
-        pixel_sum<1, V>(s, warps, 1, red[0]);
+        pixel_sum<1, V>(s, warps, red[0]);
         Vals<V> mean, rstd;
 #pragma unroll
         for (int j = 0; j < V; ++j) mean.v[j] = s[0].v[j] / (float)a.c;
         const Vals<V> minus = mul(mean, all<V>(-1.f));
         s[0] = all<V>(0.f);
         for (int ch = warp; ch < a.c; ch += warps) { const Vals<V> d = add(load(ch), minus); s[0] = fma(d, d, s[0]); }
-        pixel_sum<1, V>(s, warps, 1, red[1]);
+        pixel_sum<1, V>(s, warps, red[1]);
 #pragma unroll
         for (int j = 0; j < V; ++j) rstd.v[j] = 1.f / sqrtf(s[0].v[j] / (float)a.c + a.eps);
         if (t.live && warp == 0) {
@@ -520,8 +572,9 @@ template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_f
         for (int ch = warp; ch < a.c; ch += warps) {
             const Vals<V> x = load(ch);
             if (CK) {
-                unsigned ex;
-                const Pack<unsigned char, V> st = to_steps<T, V>(x, ex);
+                const float big = largest(x);
+                unsigned ex = step_exponent(big);
+                const Pack<unsigned char, V> st = special<T>(big) ? to_steps_special<T, V>(x, ex) : to_steps(x, ex);
                 if (t.px < a.ck.pitch) {
                     const long long run = t.n * a.c + ch;
                     store_pack<unsigned char, V>(a.ck.q + run * a.ck.pitch + t.px, st);
@@ -574,10 +627,17 @@ __device__ __forceinline__ void load_map(const NormArgs& a, const Tile& t, int c
     } else x.a = load_pack<T, V>(static_cast<const T*>(a.x) + t.n * a.x_stride + at);
 }
 
-// FULL as above.  Adds this tile's part of the warp's channel sums to dw and db of lane l for channel l.
+// FULL as above.  Adds this tile's part of the warp's channel sums to dw and db: with up to 16 channels each lane sums its pixels in
+// registers; with more, lane l gets the sums of channel l, which takes two exchanges for each value.
+template <int CPT> struct ChannelSums {
+    static constexpr bool kOwn = CPT <= 16;
+    static constexpr int kRegs = kOwn ? CPT : 1;
+    float dw[kRegs], db[kRegs];
+};
 template <class T, int V, int CPT, bool CK, bool FULL>
-__device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, int share, int number, float* red, const float2* wb, float& dw, float& db)
+__device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, int share, float* red, const float2* wb, ChannelSums<CPT>& cs)
 {
+    constexpr bool kOwn = ChannelSums<CPT>::kOwn;
     const int lane = threadIdx.x & 31, count = FULL ? CPT : t.count;
     const bool live = FULL || t.live;
     const unsigned bytes = (unsigned)a.p * sizeof(T);
@@ -606,24 +666,28 @@ __device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, 
         rstd.v[j] = live ? a.rstd[t.row + j] : 0.f;
         shift.v[j] = live ? -a.mean[t.row + j] * rstd.v[j] : 0.f;
     }
-    float sums[CPT];
+    float sums[kOwn ? 1 : CPT];
+    Vals<V> hat[CPT];
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
-        sums[i] = 0.f;
+        if (!kOwn) sums[i] = 0.f;
         if (i >= count) continue;
         const float w = wb[t.first + i].x;
-        const Vals<V> d = values(dy[i]), dh = mul(d, x[i].hats(rstd, shift));
+        hat[i] = x[i].hats(rstd, shift);
+        const Vals<V> d = values(dy[i]), dh = mul(d, hat[i]);
         s[0] = fma(d, all<V>(w), s[0]);
         s[1] = fma(dh, all<V>(w), s[1]);
-        sums[i] = sum_of(dh);
+        if constexpr (kOwn) { cs.dw[i] += sum_of(dh); cs.db[i] += sum_of(d); }
+        else sums[i] = sum_of(dh);
     }
-    if (a.partials) {
-        dw += across_lanes<CPT>(sums, lane);
+    if constexpr (!kOwn)
+        if (a.partials) {
+            cs.dw[0] += across_lanes<CPT>(sums, lane);
 #pragma unroll
-        for (int i = 0; i < CPT; ++i) sums[i] = i < count ? sum_of(values(dy[i])) : 0.f;
-        db += across_lanes<CPT>(sums, lane);
-    }
-    pixel_sum<2, V>(s, share, number, red);
+            for (int i = 0; i < CPT; ++i) sums[i] = i < count ? sum_of(values(dy[i])) : 0.f;
+            cs.db[0] += across_lanes<CPT>(sums, lane);
+        }
+    pixel_sum<2, V>(s, share, red);
     if (!a.out) return;
     const Vals<V> m0 = mul(mul(s[0], all<V>(-inv_c)), rstd), m1 = mul(mul(s[1], all<V>(-inv_c)), rstd);
     char* out = reinterpret_cast<char*>(static_cast<T*>(a.out) + t.n * a.out_stride + at);
@@ -631,10 +695,9 @@ __device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, 
     for (int i = 0; i < CPT; ++i)
         if (i < count && live)
             store_pack<T, V>(reinterpret_cast<T*>(plane(out, bytes, i)),
-                             rounded<T, V>(fma(x[i].hats(rstd, shift), m1, fma(values(dy[i]), mul(rstd, all<V>(wb[t.first + i].x)), m0))));
+                             rounded<T, V>(fma(hat[i], m1, fma(values(dy[i]), mul(rstd, all<V>(wb[t.first + i].x)), m0))));
 }
 
-// Lane l < CPT of a warp keeps the sums of the warp's channel l over all tiles of the block's group.
 template <class T, int V, int CPT, bool CK>
 __global__ void __launch_bounds__(512) norm_bwd_map_kernel(NormArgs a, int share, int per, int tiles)
 {
@@ -646,16 +709,20 @@ __global__ void __launch_bounds__(512) norm_bwd_map_kernel(NormArgs a, int share
     stage_cols(a, wb);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / share, groups = (blockDim.x >> 5) / share;
     const int half = blockDim.x * V * 2;
-    float dw = 0.f, db = 0.f;
+    ChannelSums<CPT> cs;
+#pragma unroll
+    for (int i = 0; i < ChannelSums<CPT>::kRegs; ++i) cs.dw[i] = cs.db[i] = 0.f;
     int turn = 0;
     for (long long tile = (long long)blockIdx.x * groups + group; tile < a.n * tiles; tile += (long long)gridDim.x * groups, turn ^= 1) {
         const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, (warp & (share - 1)) * per, per);
         if (t.count == CPT && t.px - lane * V + 32 * V <= a.p)
-            norm_bwd_tile<T, V, CPT, CK, true>(a, t, share, group + 1, red + turn * half, wb, dw, db);
+            norm_bwd_tile<T, V, CPT, CK, true>(a, t, share, red + turn * half, wb, cs);
         else
-            norm_bwd_tile<T, V, CPT, CK, false>(a, t, share, group + 1, red + turn * half, wb, dw, db);
+            norm_bwd_tile<T, V, CPT, CK, false>(a, t, share, red + turn * half, wb, cs);
     }
     if (!a.partials) return;
+    float dw = cs.dw[0], db = cs.db[0];
+    if constexpr (ChannelSums<CPT>::kOwn) { dw = across_lanes<CPT>(cs.dw, lane); db = across_lanes<CPT>(cs.db, lane); }
     __syncthreads();
     red[threadIdx.x] = dw;
     red[blockDim.x + threadIdx.x] = db;
@@ -706,7 +773,7 @@ template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_b
                 }
             }
         }
-        pixel_sum<2, V>(s, warps, 1, red[turn]);
+        pixel_sum<2, V>(s, warps, red[turn]);
         if (!a.out) continue;
         const Vals<V> m0 = mul(mul(s[0], all<V>(-inv_c)), rstd), m1 = mul(mul(s[1], all<V>(-inv_c)), rstd);
         for (int ch = warp; ch < a.c; ch += warps) {
@@ -743,13 +810,14 @@ __global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* partials
 // ---- host -------------------------------------------------------------------------------------------------------
 int pow2_at_least(long long v) { int r = 1; while (r < v) r <<= 1; return r; }
 
-constexpr int kMostSets = 2 * kSms;           // blocks of a backward pass, each with a partial set
+// Blocks an SM of a backward pass, each with a partial set.
+constexpr int kRowSets = 2, kMapSets = 6;
 unsigned fewer(long long a, long long b) { return (unsigned)(a < b ? a : b); }
 
 template <class T, int V, int VPT, int FORM, bool CK, int MOST> int run_fwd_rows(const NormArgs& a, int tpr, LaunchStream ls)
 {
-    const int threads = tpr > 128 ? tpr : 128, per = threads / tpr;
-    launch(norm_fwd_rows_kernel<T, V, VPT, FORM, CK, MOST>, dim3(fewer((a.rows + per - 1) / per, (long long)kSms * (1024 / threads))), dim3(threads), 0, ls, a, tpr);
+    const int threads = tpr > 32 ? tpr : 128, per = threads / tpr;
+    launch(norm_fwd_rows_kernel<T, V, VPT, FORM, CK, MOST>, dim3(fewer((a.rows + per - 1) / per, 1 << 30)), dim3(threads), 0, ls, a, tpr);
     return launched();
 }
 // 32 values to a thread where the row fills a warp that way, else one vector.
@@ -758,7 +826,7 @@ template <class T, int V, int FORM, bool CK> int pick_fwd_rows(const NormArgs& a
     const long long vecs = (a.c + (FORM == kShift ? V - 1 : 0) + V - 1) / V;
     const int least = kBlock / V < 8 ? 8 : kBlock / V;
     auto group = [&](int vpt) { const int t = pow2_at_least((vecs + vpt - 1) / vpt); return t < least ? least : t; };
-    constexpr int kWide = V == 1 ? 16 : 32 / V;
+    constexpr int kWide = V == 1 || CK ? 16 / V : 32 / V;
     if (vecs <= 32) return run_fwd_rows<T, V, 1, FORM, CK, 256>(a, group(1), ls);
     if (vecs <= kWide * 256) return run_fwd_rows<T, V, kWide, FORM, CK, 256>(a, group(kWide), ls);
     if (vecs <= kWide * 1024) return run_fwd_rows<T, V, kWide, FORM, CK, 1024>(a, group(kWide), ls);
@@ -826,7 +894,7 @@ MapShapeOf map_shape(int c, int most)
     MapShapeOf m{};
     m.share = pow2_at_least((c + most - 1) / most);
     m.per = (c + m.share - 1) / m.share;
-    m.warps = m.share > 4 ? m.share : 4;
+    m.warps = m.share > 1 ? m.share : 4;
     return m;
 }
 
@@ -837,33 +905,43 @@ template <class T, int V, bool CK> int fwd_map(const NormArgs& a, LaunchStream l
         launch(norm_fwd_long_map_kernel<T, V, CK>, dim3(fewer(all, 4 * kSms)), dim3(512), 0, ls, a, (int)tiles);
         return launched();
     }
-    const MapShapeOf m = map_shape(a.c, 32);
+    const MapShapeOf m = map_shape(a.c, a.c <= 128 && (CK || V == 2) ? 16 : 32);
     const size_t smem = (size_t)a.c * 8 + 2 * (size_t)m.warps * 32 * V * 4;
     const long long blocks = (all + m.warps / m.share - 1) / (m.warps / m.share);
-    auto go = [&](auto kernel) {
-        launch(kernel, dim3(fewer(blocks, (long long)kSms * (32 / m.warps))), dim3(m.warps * 32), smem, ls, a, m.share, m.per, (int)tiles);
-        return launched();
-    };
-    if (m.per <= 8) return go(norm_fwd_map_kernel<T, V, 8, CK, 256>);
-    return m.warps <= 8 ? go(norm_fwd_map_kernel<T, V, 32, CK, 256>) : go(norm_fwd_map_kernel<T, V, 32, CK, 1024>);
+#define GO(...)                                                                                                                             \
+    do {                                                                                                                                    \
+        launch(__VA_ARGS__, dim3(fewer(blocks, (long long)kSms * resident<__VA_ARGS__>(m.warps * 32, smem))), dim3(m.warps * 32), smem, ls, \
+               a, m.share, m.per, (int)tiles);                                                                                              \
+        return launched();                                                                                                                  \
+    } while (0)
+    if (m.per <= 8 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 8, CK, 256>);
+    if constexpr (CK || V == 2)
+        if (m.per <= 16 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 16, CK, 256>);
+    if (m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 32, CK, 256>);
+    GO(norm_fwd_map_kernel<T, V, 32, CK, 1024>);
+#undef GO
 }
 template <class T, int V, bool CK> int bwd_map(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
     const long long tiles = (a.p + 32 * V - 1) / (32 * V), all = a.n * tiles;
     if (a.c > 512) {
-        const int blocks = fewer(all, kMostSets);
+        const int blocks = fewer(all, 2 * kSms);
         launch(norm_bwd_long_map_kernel<T, V, CK>, dim3(blocks), dim3(512 / V), 0, ls, a, (int)tiles);
         return sum_sets(a, blocks, dweight, dbias, ls);
     }
-    MapShapeOf m = map_shape(a.c, a.c <= 256 ? 16 : 32);
-    m.warps = m.share > 8 ? m.share : 8;
+    const MapShapeOf m = map_shape(a.c, CK && V == 2 && a.c <= 128 ? 8 : a.c <= 256 ? 16 : 32);
     const size_t smem = (size_t)a.c * 8 + 4 * (size_t)m.warps * 32 * V * 4;
-    const int blocks = fewer((all + m.warps / m.share - 1) / (m.warps / m.share), (long long)kSms * (16 / m.warps));
-    auto go = [&](auto kernel) {
-        launch(kernel, dim3(blocks), dim3(m.warps * 32), smem, ls, a, m.share, m.per, (int)tiles);
-        return sum_sets(a, blocks, dweight, dbias, ls);
-    };
-    return m.per <= 8 ? go(norm_bwd_map_kernel<T, V, 8, CK>) : m.per <= 16 ? go(norm_bwd_map_kernel<T, V, 16, CK>) : go(norm_bwd_map_kernel<T, V, 32, CK>);
+    const long long want = (all + m.warps / m.share - 1) / (m.warps / m.share);
+#define GO(...)                                                                                                    \
+    do {                                                                                                           \
+        const int fit = resident<__VA_ARGS__>(m.warps * 32, smem), blocks = fewer(want, (long long)kSms * (fit < kMapSets ? fit : kMapSets)); \
+        launch(__VA_ARGS__, dim3(blocks), dim3(m.warps * 32), smem, ls, a, m.share, m.per, (int)tiles);            \
+        return sum_sets(a, blocks, dweight, dbias, ls);                                                            \
+    } while (0)
+    if (m.per <= 8) GO(norm_bwd_map_kernel<T, V, 8, CK>);
+    if (m.per <= 16) GO(norm_bwd_map_kernel<T, V, 16, CK>);
+    GO(norm_bwd_map_kernel<T, V, 32, CK>);
+#undef GO
 }
 
 // Whether arrays can be read as pairs of 16-bit pixels.
@@ -893,7 +971,7 @@ template <class T> int backward(const NormArgs& a, bool ck, float* dw, float* db
     return ck ? backward<T, true>(a, dw, db, ls) : backward<T, false>(a, dw, db, ls);
 }
 
-size_t workspace_bytes(const ftp_dims* d) { return (size_t)kMostSets * 2 * (size_t)d->c * 4; }
+size_t workspace_bytes(const ftp_dims* d) { return (size_t)kSms * (d->p == 1 ? kRowSets : kMapSets) * 2 * (size_t)d->c * 4; }
 
 }  // namespace
 

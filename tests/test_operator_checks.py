@@ -68,7 +68,7 @@ def _norm_backward(d=None, x=SOME, xs=0, k=None, dy=SOME, dys=0, w=None, m=SOME,
 
 
 @pytest.mark.parametrize("bad", [dict(x=None), dict(k=SOME), dict(x=None, k=SOME + 8), dict(dy=None), dict(m=None), dict(r=None), dict(dw=None),
-                                 dict(db=None), dict(dx=None, dw=None, db=None), dict(ws=None), dict(ws=SOME + 8), dict(n=4 * 148 * 2 * 8 * 4 - 1),
+                                 dict(db=None), dict(dx=None, dw=None, db=None), dict(ws=None), dict(ws=SOME + 8), dict(n=2 * 148 * 2 * 8 * 4 - 1),
                                  dict(xs=7), dict(dys=7), dict(dxs=7), dict(dy=SOME + 2), dict(dx=SOME + 2), dict(w=SOME + 2),
                                  dict(dw=SOME + 2), dict(db=SOME + 2), dict(m=SOME + 2), dict(r=SOME + 2)])
 def test_norm_backward_refuses(bad):
