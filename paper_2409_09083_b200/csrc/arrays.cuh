@@ -61,6 +61,20 @@ template <class T, int V> __device__ __forceinline__ Pack<T, V> zero_pack()
     return r;
 }
 
+// Keeps 16-bit values packed: without it the compiler holds on to their fp32 forms between two passes, in twice the registers.
+template <class T, int V> __device__ __forceinline__ void keep_packed(Pack<T, V>& a)
+{
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            unsigned w;
+            __builtin_memcpy(&w, &a.v[j], 4);
+            asm volatile("" : "+r"(w));
+            __builtin_memcpy(&a.v[j], &w, 4);
+        }
+    }
+}
+
 // Values [e, e + V) of an array of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as 0
 // and is not written.
 template <class T, int V> __device__ __forceinline__ Pack<T, V> load_part(const T* base, long long e, long long lo, long long hi)

@@ -8,6 +8,7 @@
 // The variance is the mean of (x - mean)^2 over values in registers, not E x^2 - mean^2.  dweight and dbias: a thread (in maps: a lane)
 // keeps the same columns for all its rows and sums them in registers; each block writes one partial set and a second launch adds the
 // sets in a fixed order.
+#include <algorithm>
 #include "arrays.cuh"
 
 using namespace ftp;
@@ -98,99 +99,99 @@ template <class T, int V> struct Raw<T, V, true> {
 // the 16-byte grid below the row's start (x and y the same distance above it); then column = place - o.  With V = 1 any alignment goes.
 enum { kFast, kEdge, kShift };
 
+// Values wait in registers as they were read and are widened again in each of the three passes: with 8 vectors a thread a warp holds
+// 2048 values of 16 bits, and exchanges, barriers and addresses are shared by 64 values of each lane.
 template <class T, int V, int VPT, int FORM, bool CK, int MOST>
-__global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_rows_kernel(NormArgs a, int tpr)
+__global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel(NormArgs a, int tpr)
 {
     constexpr bool kWhole = FORM == kFast || V == 1;
-    constexpr int E = V * VPT;
-    __shared__ float red[2][32];
+    __shared__ float red[2][16];
     previous_launches();
-    const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = threadIdx.x / tpr;
+    const int per = tpr > 32 ? 1 : blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = tpr > 32 ? 0 : threadIdx.x / tpr;
     const float inv_c = 1.f / (float)a.c;
-    for (long long row0 = (long long)blockIdx.x * per; row0 < a.rows; row0 += (long long)gridDim.x * per) {
+    const long long step = (long long)gridDim.x * per;
+    for (long long row0 = (long long)blockIdx.x * per; row0 < a.rows; row0 += step) {
         const long long row = row0 + group;
         const bool live = row < a.rows;
         const T* xr = static_cast<const T*>(a.x) + row * a.x_stride;
         const int o = FORM == kShift ? (int)((reinterpret_cast<uintptr_t>(xr) / sizeof(T)) & (V - 1)) : 0;
         const int hi = live ? o + a.c : 0;
-        xr -= o;
+        xr += t * V - o;
         Pack<T, V> raw[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
             raw[i] = zero_pack<T, V>();
-            if (e < hi) raw[i] = kWhole ? load_pack<T, V>(xr + e) : load_part<T, V>(xr, e, o, hi);
+            if (e < hi) raw[i] = kWhole ? load_pack<T, V>(xr + i * tpr * V) : load_part<T, V>(xr - t * V, e, o, hi);
         }
-        Vals<E> x;
+        Vals<V> acc = values(raw[0]);
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const Vals<V> v = values(raw[i]);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x.v[i * V + j] = v.v[j];
-        }
-        float s[1] = {sum_of(x)};
+        for (int i = 1; i < VPT; ++i) acc = add(acc, values(raw[i]));
+        float s[1] = {sum_of(acc)};
         group_sum<1>(s, tpr, 0, red[0]);
         const float mean = a.c == 1 ? s[0] : s[0] * inv_c;
+        acc = all<V>(0.f);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) keep_packed(raw[i]);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            const float minus = e < hi ? -mean : 0.f;           // (a vector that is not there stays 0)
-            Vals<V> v;
-#pragma unroll
-            for (int j = 0; j < V; ++j) v.v[j] = x.v[i * V + j];
-            v = add(v, all<V>(minus));
-            if (!kWhole && (e < o || e + V > hi)) {             // nor places before or behind the row
+            Vals<V> d = add(values(raw[i]), all<V>(e < hi ? -mean : 0.f));       // (a vector that is not there stays 0)
+            if (!kWhole && (e < o || e + V > hi)) {                               // nor places before or behind the row
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    if (e + j < o || e + j >= hi) v.v[j] = 0.f;
+                    if (e + j < o || e + j >= hi) d.v[j] = 0.f;
             }
-#pragma unroll
-            for (int j = 0; j < V; ++j) x.v[i * V + j] = v.v[j];
+            acc = fma(d, d, acc);
         }
-        s[0] = sum_of(mul(x, x));
+        s[0] = sum_of(acc);
         group_sum<1>(s, tpr, 0, red[1]);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) keep_packed(raw[i]);
         const float rstd = 1.f / sqrtf(s[0] * inv_c + a.eps);
         if (live && t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
-        T* yr = static_cast<T*>(a.out) + row * a.out_stride - o;
+        T* yr = static_cast<T*>(a.out) + row * a.out_stride + t * V - o;
+        unsigned char* qr = a.ck.q + row * a.ck.pitch + t * V;
+        unsigned char* er = a.ck.steps + row * a.ck.blocks + t * V / kBlock;
         bool any = false;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int e = (i * tpr + t) * V;
+            const int skip = i * tpr * V, e = skip + t * V;
+            const Vals<V> v = values(raw[i]);
             if (CK) {                                           // as if all values were finite
-                const Vals<V> v = values(raw[i]);
                 const float big = largest(v);
                 any |= special<T>(big);
                 const unsigned ex = step_exponent(big);
                 if (live && e < a.ck.pitch) {
-                    store_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e, to_steps(v, ex));
-                    if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
+                    store_pack<unsigned char, V>(qr + skip, to_steps(v, ex));
+                    if (e % kBlock == 0) er[skip / kBlock] = (unsigned char)ex;
                 }
             }
             if (e < hi) {
-                Vals<V> w, b, v;
+                Vals<V> w, b;
                 load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v);
                 load_cols<FORM == kFast, V>(a.bias, e - o, a.c, 0.f, b.v);
-#pragma unroll
-                for (int j = 0; j < V; ++j) v.v[j] = x.v[i * V + j];
-                const Pack<T, V> y = rounded<T, V>(fma(mul(v, all<V>(rstd)), w, b));
-                if (kWhole) store_pack<T, V>(yr + e, y);
-                else store_part<T, V>(yr, e, o, hi, y);
+                const Pack<T, V> y = rounded<T, V>(fma(mul(add(v, all<V>(-mean)), all<V>(rstd)), w, b));
+                if (kWhole) store_pack<T, V>(yr + skip, y);
+                else store_part<T, V>(yr - t * V, e, o, hi, y);
             }
         }
         if (CK && __any_sync(0xffffffffu, any)) {               // the blocks with others once more
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < VPT; ++i) {
-                const int e = (i * tpr + t) * V;
-                const Vals<V> v = values(raw[i]);
+                const int skip = i * tpr * V, e = skip + t * V;
+                Pack<T, V> again = zero_pack<T, V>();
+                if (e < hi) again = load_part<T, V>(xr - t * V, e, 0, hi);
+                const Vals<V> v = values(again);
                 if (!special<T>(largest(v))) continue;
                 unsigned ex;
                 const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
                 if (live && e < a.ck.pitch) {
-                    store_pack<unsigned char, V>(a.ck.q + row * a.ck.pitch + e, st);
-                    if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
+                    store_pack<unsigned char, V>(qr + skip, st);
+                    if (e % kBlock == 0) er[skip / kBlock] = (unsigned char)ex;
                 }
             }
         }
@@ -471,9 +472,13 @@ __device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, 
     const Vals<V> mean = a.c == 1 ? s[0] : mul(s[0], all<V>(inv_c)), minus = mul(mean, all<V>(-1.f));
     s[0] = all<V>(0.f);
 #pragma unroll
+    for (int i = 0; i < CPT; ++i) keep_packed(raw[i]);
+#pragma unroll
     for (int i = 0; i < CPT; ++i)
         if (i < count) { const Vals<V> d = add(values(raw[i]), minus); s[0] = fma(d, d, s[0]); }
     pixel_sum<1, V>(s, share, red + half);
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) keep_packed(raw[i]);
     Vals<V> rstd;
 #pragma unroll
     for (int j = 0; j < V; ++j) rstd.v[j] = 1.f / sqrtf(s[0].v[j] * inv_c + a.eps);
@@ -814,22 +819,24 @@ int pow2_at_least(long long v) { int r = 1; while (r < v) r <<= 1; return r; }
 constexpr int kRowSets = 2, kMapSets = 6;
 unsigned fewer(long long a, long long b) { return (unsigned)(a < b ? a : b); }
 
-template <class T, int V, int VPT, int FORM, bool CK, int MOST> int run_fwd_rows(const NormArgs& a, int tpr, LaunchStream ls)
+template <class T, int V, int VPT, int FORM, bool CK, int MOST = 128> int run_fwd_rows(const NormArgs& a, int tpr, LaunchStream ls)
 {
-    const int threads = tpr > 32 ? tpr : 128, per = threads / tpr;
-    launch(norm_fwd_rows_kernel<T, V, VPT, FORM, CK, MOST>, dim3(fewer((a.rows + per - 1) / per, 1 << 30)), dim3(threads), 0, ls, a, tpr);
+    const int threads = tpr > 32 ? tpr : 128, per = tpr > 32 ? 1 : threads / tpr;
+    const long long fit = (long long)kSms * resident<norm_fwd_rows_kernel<T, V, VPT, FORM, CK, MOST>>(threads, 0);
+    launch(norm_fwd_rows_kernel<T, V, VPT, FORM, CK, MOST>, dim3(fewer((a.rows + per - 1) / per, fit)), dim3(threads), 0, ls, a, tpr);
     return launched();
 }
-// 32 values to a thread where the row fills a warp that way, else one vector.
+// As many vectors to a thread as let a warp hold the row, up to 8 (128 bytes a thread as read); then more warps.
 template <class T, int V, int FORM, bool CK> int pick_fwd_rows(const NormArgs& a, LaunchStream ls)
 {
     const long long vecs = (a.c + (FORM == kShift ? V - 1 : 0) + V - 1) / V;
     const int least = kBlock / V < 8 ? 8 : kBlock / V;
     auto group = [&](int vpt) { const int t = pow2_at_least((vecs + vpt - 1) / vpt); return t < least ? least : t; };
-    constexpr int kWide = V == 1 || CK ? 16 / V : 32 / V;
-    if (vecs <= 32) return run_fwd_rows<T, V, 1, FORM, CK, 256>(a, group(1), ls);
-    if (vecs <= kWide * 256) return run_fwd_rows<T, V, kWide, FORM, CK, 256>(a, group(kWide), ls);
-    if (vecs <= kWide * 1024) return run_fwd_rows<T, V, kWide, FORM, CK, 1024>(a, group(kWide), ls);
+    constexpr int kWide = V == 1 ? 32 : 8;
+    if (vecs <= 32) return run_fwd_rows<T, V, 1, FORM, CK>(a, group(1), ls);
+    if (vecs <= 4 * 32) return run_fwd_rows<T, V, 4, FORM, CK>(a, 32, ls);
+    if (vecs <= kWide * 128) return run_fwd_rows<T, V, kWide, FORM, CK>(a, group(kWide) < 32 ? 32 : group(kWide), ls);
+    if (vecs <= kWide * 512) return run_fwd_rows<T, V, kWide, FORM, CK, 512>(a, group(kWide), ls);
     launch(norm_fwd_long_rows_kernel<T, CK>, dim3(fewer(a.rows, 2 * kSms)), dim3(1024), 0, ls, a);
     return launched();
 }
@@ -910,10 +917,13 @@ template <class T, int V, bool CK> int fwd_map(const NormArgs& a, LaunchStream l
     const long long blocks = (all + m.warps / m.share - 1) / (m.warps / m.share);
 #define GO(...)                                                                                                                             \
     do {                                                                                                                                    \
-        launch(__VA_ARGS__, dim3(fewer(blocks, (long long)kSms * resident<__VA_ARGS__>(m.warps * 32, smem))), dim3(m.warps * 32), smem, ls, \
+        launch(__VA_ARGS__, dim3(fewer(blocks, (long long)kSms * std::min(cap, resident<__VA_ARGS__>(m.warps * 32, smem)))), dim3(m.warps * 32), smem, ls, \
                a, m.share, m.per, (int)tiles);                                                                                              \
         return launched();                                                                                                                  \
     } while (0)
+    // 16 warps an SM with 32 loads each on their way: with 20 and 24 the map of 16 x 32 x 304 x 304 takes 72 and 74 us instead of 64.  With
+    // a checkpoint to write the kernel is closer to the issue rate and takes all it can get (123 us with 16 warps, 111 with 24).
+    const int cap = CK ? 32 : 16 / m.warps > 0 ? 16 / m.warps : 1;
     if (m.per <= 8 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 8, CK, 256>);
     if constexpr (CK || V == 2)
         if (m.per <= 16 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 16, CK, 256>);
