@@ -75,16 +75,28 @@ template <class T, int V> __device__ __forceinline__ void keep_packed(Pack<T, V>
     }
 }
 
-// Values [e, e + V) of an array of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as 0
-// and is not written.
-template <class T, int V> __device__ __forceinline__ Pack<T, V> load_part(const T* base, long long e, long long lo, long long hi)
+// Values [e, e + V) of an array of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as `fill`
+// and is not written.  Loads come in two steps: load_whole of all a thread's words, each one predicated instruction, then load_rest
+// where a word lies across an end.  (One function with both would put a branch between any two loads, and the next would not be
+// issued before the last has arrived.)
+template <class T, int V> __device__ __forceinline__ Pack<T, V> filled(T fill)
 {
-    if (e >= lo && e + V <= hi) return load_pack<T, V>(base + e);
-    Pack<T, V> r = zero_pack<T, V>();
+    Pack<T, V> r;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-        if (e + j >= lo && e + j < hi) r.v[j] = base[e + j];
+    for (int j = 0; j < V; ++j) r.v[j] = fill;
     return r;
+}
+template <class T, int V> __device__ __forceinline__ void load_whole(Pack<T, V>& r, const T* base, long long e, long long lo, long long hi)
+{
+    if (e >= lo && e + V <= hi) r = load_pack<T, V>(base + e);
+}
+template <class T, int V> __device__ __forceinline__ void load_rest(Pack<T, V>& r, const T* base, long long e, long long lo, long long hi)
+{
+    if (V > 1 && e < hi && e + V > lo && (e < lo || e + V > hi)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (e + j >= lo && e + j < hi) r.v[j] = base[e + j];
+    }
 }
 template <class T, int V> __device__ __forceinline__ void store_part(T* base, long long e, long long lo, long long hi, const Pack<T, V>& a)
 {

@@ -45,7 +45,12 @@ template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads)
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
                 const long long e = first + i * 32 * V;
-                raw[i] = e < a.len ? load_part<T, V>(x, e, 0, a.len) : zero_pack<T, V>();
+                raw[i] = zero_pack<T, V>();
+                load_whole<T, V>(raw[i], x, e, 0, a.len);
+            }
+            if (a.len % V) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) load_rest<T, V>(raw[i], x, first + i * 32 * V, 0, a.len);
             }
             // every block as if it held finite values only, then the others again
             bool any = false;

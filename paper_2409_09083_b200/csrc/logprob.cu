@@ -23,6 +23,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -160.f;                       // 2^-160 is 0 in fp32: where a = -inf would make 0 * inf
 constexpr int kTop = FTP_TOP_MAX;
 constexpr int kParts = 32;                             // parts of a row, whose maxima bound its best values
+constexpr int kBlockThreads = 256;
 constexpr int kListBlock = 512, kListWarp = 64;        // candidates
 constexpr int kCountHere = 4096;                       // rows whose labels every block counts by itself
 
@@ -118,15 +119,6 @@ __device__ __forceinline__ void write_stats(const LpArgs& a, long long row, cons
     if (a.entropy) a.entropy[row] = r.entropy;
 }
 
-template <class T, int V> __device__ __forceinline__ Pack<T, V> load_logits(const T* base, int e, int lo, int hi)
-{
-    if (e >= lo && e + V <= hi) return load_pack<T, V>(base + e);
-    Pack<T, V> r;
-#pragma unroll
-    for (int j = 0; j < V; ++j) r.v[j] = e + j >= lo && e + j < hi ? base[e + j] : from_f<T>(minus_inf());
-    return r;
-}
-
 // (z - m) log2 e.  The difference comes first: logits of the type's lowest value, which masks use, would overflow otherwise.
 __device__ __forceinline__ float exponent_of(float z, float m) { return (z - m) * kLog2e; }
 
@@ -146,19 +138,62 @@ __device__ __forceinline__ float labelled_rows(const LpArgs& a)
 }
 
 // ---- matrices ---------------------------------------------------------------------------------------------------
+// Largest value of packs, two 16-bit values to an instruction; NaNs are passed over.
+template <class T, int V> struct Largest {
+    float v = minus_inf();
+    __device__ __forceinline__ void take(const Pack<T, V>& p)
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v = fmaxf(v, to_f(p.v[j]));
+    }
+    __device__ __forceinline__ float value() const { return v; }
+};
+__device__ __forceinline__ __nv_bfloat162 max_two(__nv_bfloat162 a, __nv_bfloat162 b) { return __hmax2(a, b); }
+__device__ __forceinline__ __half2 max_two(__half2 a, __half2 b) { return __hmax2(a, b); }
+template <class T, class T2> struct LargestPairs {
+    T2 v;
+    __device__ __forceinline__ LargestPairs() { v.x = v.y = from_f<T>(minus_inf()); }
+    __device__ __forceinline__ void take(const Pack<T, 8>& p)
+    {
+        T2 w[4];
+        __builtin_memcpy(w, &p, 16);
+        v = max_two(v, max_two(max_two(w[0], w[1]), max_two(w[2], w[3])));
+    }
+    __device__ __forceinline__ float value() const { return fmaxf(to_f(v.x), to_f(v.y)); }
+};
+template <> struct Largest<__nv_bfloat16, 8> : LargestPairs<__nv_bfloat16, __nv_bfloat162> {};
+template <> struct Largest<__half, 8> : LargestPairs<__half, __half2> {};
+
+// Order of fp32 values as unsigned numbers (no NaNs).
+__device__ __forceinline__ unsigned order_of(float v)
+{
+    const unsigned b = __float_as_uint(v + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+// A bound that `top` of the 32 lanes' values reach at least: the maximum, taken away `top` - 1 times with all that are equal to it.
+__device__ __forceinline__ float bound_of(float v, int top)
+{
+    unsigned mine = order_of(v), best = 0;
+    for (int k = 0; k < top; ++k) {
+        best = __reduce_max_sync(0xffffffffu, mine);
+        if (best == order_of(minus_inf())) break;
+        if (mine == best) mine = order_of(minus_inf());
+    }
+    return __uint_as_float(best & 0x80000000u ? best & 0x7fffffffu : ~best);
+}
+
 // A group of TPR threads (a warp, or the block) holds a row, or with a cluster its part of one, as NV vectors of V logits a
 // thread.  SHIFT as in norm.cu: vectors lie on the 16-byte grid below the row's start.
 template <int TPR> struct RowShared {
-    static constexpr int kGroups = TPR == 32 ? 8 : 1;
+    static constexpr int kGroups = TPR == 32 ? kBlockThreads / 32 : 1;
     static constexpr int kList = TPR == 32 ? kListWarp : kListBlock;
     unsigned long long list[kGroups][kList];
     unsigned long long best[kTop];           // a block's own best, for the cluster
-    float parts[kParts];
-    float bound;
-    float red[2][32];
-    int count[kGroups];
     unsigned long long round[32];
-    Sums sums;
+    float parts[kParts];
+    Sums sums[2][32];                        // of the warps; of this row and the one before
+    int count[2][kGroups];
+    Sums whole;
 };
 
 // The `top` best of `m` keys in `list`, by counting; write(place, key) for each.
@@ -172,132 +207,148 @@ template <int TPR, class F> __device__ __forceinline__ void place(const unsigned
     }
 }
 
+// Sums of `n` warps, a power of two up to 32; every lane has them.
+__device__ __forceinline__ Sums join_lanes(const Sums* of, int n)
+{
+    const int lane = threadIdx.x & 31;
+    Sums s = of[lane & (n - 1)];
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1)
+        if (d < n) {
+            const Sums o{__shfl_xor_sync(0xffffffffu, s.m, d), __shfl_xor_sync(0xffffffffu, s.s, d), __shfl_xor_sync(0xffffffffu, s.t, d)};
+            s = lane & d ? join(o, s) : join(s, o);            // (the same bits in all lanes)
+        }
+    return s;
+}
+
 template <class T, int V, int NV, int TPR, bool SHIFT, int MODE>
-__global__ void __launch_bounds__(TPR == 32 ? 256 : 512) logprob_rows_kernel(LpArgs a, int cluster, int part)
+__global__ void __launch_bounds__(kBlockThreads, NV * sizeof(Pack<T, V>) > 128 && (sizeof(T) == 4 || V == 1) ? 1 : 2) logprob_rows_kernel(LpArgs a, int cluster, int part)
 {
     __shared__ RowShared<TPR> sh;
     previous_launches();
-    constexpr int kGroups = RowShared<TPR>::kGroups;
+    constexpr int kGroups = RowShared<TPR>::kGroups, kWarps = TPR / 32;
     const int t = threadIdx.x & (TPR - 1), group = threadIdx.x / TPR, lane = threadIdx.x & 31;
     const int rank = TPR == 32 ? 0 : (int)(blockIdx.x % cluster);
     const long long step = (long long)(gridDim.x / cluster) * kGroups;
+    const bool want_top = MODE == kStats && a.top > 0;
     float over = 0.f, total = 0.f;
     if (MODE == kLoss) {
         const float k = labelled_rows(a);
         over = k > 0.f ? a.scale / k : 0.f;
     }
-    for (long long row0 = (long long)(blockIdx.x / cluster) * kGroups; row0 < a.rows; row0 += step) {
-        const long long row = row0 + group;
-        if (TPR == 32 && row >= a.rows) break;                   // (a warp of its own: nobody waits for it)
+    Pack<T, V> raw[NV];
+    auto load_row = [&](long long row) {
         const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
         const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0;
-        const int hi = o + a.c, first = rank * part, last = min(hi, first + part);
-        Label label{-1, 0.f, 0};
-        label = read_label<T>(a, row, zr, 1);
+        const int first = rank * part, last = min(o + a.c, first + part);
         zr -= o;
-        Pack<T, V> raw[NV];
-        float big = minus_inf();
 #pragma unroll
-        for (int i = 0; i < NV; ++i) raw[i] = load_logits<T, V>(zr, first + (i * TPR + t) * V, o, last);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) big = fmaxf(big, to_f(raw[i].v[j]));
-        // the row's maximum, and the parts' ones
-        float part_max = big, m;
-        if (TPR == 32) m = lanes_max(big, 32);
-        else {
-            part_max = lanes_max(big, TPR / kParts);
-            if (t % (TPR / kParts) == 0) sh.parts[t / (TPR / kParts)] = part_max;
-            if (t == 0) sh.count[0] = 0;
-            __syncthreads();
-            part_max = sh.parts[lane];
-            m = lanes_max(part_max, 32);
+        for (int i = 0; i < NV; ++i) {
+            raw[i] = filled<T, V>(from_f<T>(minus_inf()));
+            load_whole<T, V>(raw[i], zr, first + (i * TPR + t) * V, o, last);
         }
-        if (TPR == 32) {
-            if (lane == 0) sh.count[group] = 0;
-            __syncwarp();
-        }
-        float bound = minus_inf();
-        const bool want_top = MODE == kStats && a.top > 0;
-        if (want_top && (TPR == 32 || t < 32)) {
-            int better = 0;
+        if (SHIFT || a.c % V) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const float v = __shfl_sync(0xffffffffu, part_max, i);
-                better += v > part_max || (v == part_max && i < lane);
-            }
-            const unsigned who = __ballot_sync(0xffffffffu, better == a.top - 1);
-            bound = __shfl_sync(0xffffffffu, part_max, __ffs(who) - 1);
-            if (TPR != 32 && t == 0) sh.bound = bound;
+            for (int i = 0; i < NV; ++i) load_rest<T, V>(raw[i], zr, first + (i * TPR + t) * V, o, last);
         }
-        const float shift = m == minus_inf() ? 0.f : m;
-        float s = 0.f, tt = 0.f;
+    };
+    long long row = (long long)(blockIdx.x / cluster) * kGroups + group;
+    if (row < a.rows) load_row(row);
+    if (threadIdx.x < 2 * kGroups) sh.count[threadIdx.x / kGroups][threadIdx.x % kGroups] = 0;
+    __syncthreads();
+    int turn = 0;
+    for (; row < a.rows; row += step, turn ^= 1) {              // (a warp's own rows, or the whole block's or cluster's)
+        const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
+        const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0;
+        const int first = rank * part, last = min(o + a.c, first + part);
+        Label label{-1, 0.f, 0};
+        if (MODE == kLoss || t == 0) label = read_label<T>(a, row, zr, 1);
+        Largest<T, V> most;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) most.take(raw[i]);
+        const float mine = most.value();
+        // largest of a part of the row, and of the warp, which the exponents are taken from
+        constexpr int kLanes = TPR / kParts;                    // of a part
+        float part_max = lanes_max(mine, kLanes);
+        if (TPR != 32 && want_top && lane % kLanes == 0) sh.parts[t / kLanes] = part_max;
+        const float m = lanes_max(part_max), shift = m == minus_inf() ? 0.f : m;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) keep_packed(raw[i]);
+        Vals<V> s = all<V>(0.f), x2 = all<V>(0.f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            Vals<V> x = mul(add(values(raw[i]), all<V>(-shift)), all<V>(kLog2e)), e;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float x = max_nan(exponent_of(to_f(raw[i].v[j]), shift), kLeast), e = ex2(x);
-                s += e;
-                if (MODE == kStats) tt = fmaf(e, x, tt);
+                if (MODE == kStats) x.v[j] = max_nan(x.v[j], kLeast);
+                e.v[j] = ex2(x.v[j]);
             }
-        s = lanes_sum(s, 32);
-        if (MODE == kStats) tt = lanes_sum(tt, 32);
-        if (TPR != 32) {
-            if (lane == 0) { sh.red[0][t >> 5] = s; sh.red[1][t >> 5] = tt; }
-            __syncthreads();
-            s = lanes_sum(lane < TPR / 32 ? sh.red[0][lane] : 0.f, 32);
-            if (MODE == kStats) tt = lanes_sum(lane < TPR / 32 ? sh.red[1][lane] : 0.f, 32);
-            bound = sh.bound;
+            s = add(s, e);
+            if (MODE == kStats) x2 = fma(e, x, x2);
         }
-        Sums sums{shift, s, tt};
+        Sums sums{shift, lanes_sum(sum_of(s)), 0.f};
+        if (MODE == kStats) sums.t = lanes_sum(sum_of(x2));
+        if (TPR != 32) {
+            if (lane == 0) sh.sums[turn][t >> 5] = sums;
+            __syncthreads();
+            if (t < 32 || MODE == kLoss || cluster > 1) sums = join_lanes(sh.sums[turn], kWarps);
+            part_max = sh.parts[lane];
+        }
+        if (t == 0) sh.count[turn ^ 1][group] = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) keep_packed(raw[i]);
         // the best classes of this part
         int found = 0;
         if (want_top) {
-            if (big >= bound) {
+            const float bound = bound_of(part_max, a.top);
+            if (mine >= bound) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
+                    Largest<T, V> here;
+                    here.take(raw[i]);
+                    if (here.value() < bound) continue;
                     const int e = first + (i * TPR + t) * V;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float v = fmaxf(to_f(raw[i].v[j]), minus_inf());
                         if (v >= bound && e + j >= o && e + j < last) {
-                            const int at = atomicAdd(&sh.count[group], 1);
+                            const int at = atomicAdd(&sh.count[turn][group], 1);
                             if (at < RowShared<TPR>::kList) sh.list[group][at] = key_of(v, e + j - o);
                         }
                     }
                 }
             }
             if (TPR == 32) __syncwarp(); else __syncthreads();
-            found = sh.count[group];
+            found = sh.count[turn][group];
             if (found > RowShared<TPR>::kList) {                  // too many equal ones: one place after the other
                 unsigned long long before = ~0ull;
                 const int places = min(a.top, found);
                 for (int k = 0; k < places; ++k) {
-                    unsigned long long mine = 0;
+                    unsigned long long best = 0;
 #pragma unroll
                     for (int i = 0; i < NV; ++i) {
                         const int e = first + (i * TPR + t) * V;
 #pragma unroll
                         for (int j = 0; j < V; ++j) {
                             const unsigned long long key = e + j >= o && e + j < last ? key_of(to_f(raw[i].v[j]), e + j - o) : 0ull;
-                            if (key < before && key > mine) mine = key;
+                            if (key < before && key > best) best = key;
                         }
                     }
-                    mine = lanes_best(mine, 32);
+                    best = lanes_best(best, 32);
                     if (TPR != 32) {
                         __syncthreads();
-                        if (lane == 0) sh.round[t >> 5] = mine;
+                        if (lane == 0) sh.round[t >> 5] = best;
                         __syncthreads();
-                        mine = lanes_best(lane < TPR / 32 ? sh.round[lane] : 0ull, 32);
+                        best = lanes_best(lane < kWarps ? sh.round[lane] : 0ull, 32);
                     }
-                    before = mine;
-                    if (t == 0) sh.list[group][k] = mine;
+                    before = best;
+                    if (t == 0) sh.list[group][k] = best;
                 }
                 found = places;
                 if (TPR == 32) __syncwarp(); else __syncthreads();
             }
         }
+        if (MODE == kStats && row + step < a.rows) load_row(row + step);       // on their way while this row's results are written
         if (TPR != 32 && cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (want_top) {
@@ -305,10 +356,10 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : 512) logprob_rows_kernel(LpA
                 __syncthreads();
                 place<TPR>(sh.list[0], found, a.top, t, [&](int at, unsigned long long k) { sh.best[at] = k; });
             }
-            if (t == 0) sh.sums = sums;
+            if (t == 0) sh.whole = sums;
             cl.sync();
-            sums = *cl.map_shared_rank(&sh.sums, 0);
-            for (int r = 1; r < cluster; ++r) sums = join(sums, *cl.map_shared_rank(&sh.sums, r));
+            sums = *cl.map_shared_rank(&sh.whole, 0);
+            for (int r = 1; r < cluster; ++r) sums = join(sums, *cl.map_shared_rank(&sh.whole, r));
             if (want_top && rank == 0) {
                 found = cluster * a.top;
                 for (int i = t; i < found; i += TPR) sh.list[0][i] = cl.map_shared_rank(sh.best, i / a.top)[i % a.top];
@@ -318,41 +369,44 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : 512) logprob_rows_kernel(LpA
         const RowResult r = result_of(sums);
         if (MODE == kStats && rank == 0) {
             if (t == 0) write_stats(a, row, r, label);
-            if (want_top)
-                place<TPR>(sh.list[group], found, a.top, t, [&](int at, unsigned long long k) {
-                    if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
-                    if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
-                });
+            auto best_of_row = [&](int at, unsigned long long k) {
+                if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
+                if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
+            };
+            if (want_top && TPR != 32 && cluster > 1) place<TPR>(sh.list[0], found, a.top, t, best_of_row);
+            else if (want_top && t < 32) place<32>(sh.list[group], found, a.top, t, best_of_row);     // (this warp alone knows the row's sums)
         }
         if (MODE == kLoss) {
             if (t == 0 && rank == 0 && label.has) total += logp_of_label(r, label);
             if (a.dz) {
                 T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
                 const float f = label.has > 0 ? (r.empty ? 0.f : over) : label.has == 0 ? 0.f : nan_f();
-                const float g = f / sums.s;
-                const bool nothing = f == 0.f;
+                const float g = f == 0.f ? 0.f : f / sums.s;
                 const int at = label.has > 0 ? (int)label.cls + o : -1;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const int e = first + (i * TPR + t) * V;
                     if (e >= last) continue;
-                    Pack<T, V> d;
+                    Vals<V> x = mul(add(values(raw[i]), all<V>(-sums.m)), all<V>(kLog2e));
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float x = ex2(exponent_of(to_f(raw[i].v[j]), sums.m)) * g;
-                        d.v[j] = from_f<T>(nothing ? 0.f : e + j == at ? x - f : x);
+                    for (int j = 0; j < V; ++j) x.v[j] = ex2(x.v[j]);
+                    x = mul(x, all<V>(g));
+                    if (f == 0.f) x = all<V>(0.f);              // (whatever the logits are)
+                    if ((unsigned)(at - e) < (unsigned)V) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            if (e + j == at) x.v[j] -= f;
                     }
-                    store_part<T, V>(dr, e, o, last, d);
+                    store_part<T, V>(dr, e, o, last, rounded<T, V>(x));
                 }
             }
+            if (row + step < a.rows) load_row(row + step);
         }
-        if (TPR != 32) {                                  // before the next row's values take the places of these
-            if (cluster > 1) cg::this_cluster().sync();
-            else __syncthreads();
-        } else __syncwarp();
+        if (TPR != 32 && cluster > 1) cg::this_cluster().sync();       // the others read this block's part
+        if (TPR == 32) __syncwarp();
     }
     if (MODE == kLoss && a.sums) {
-        __shared__ float red[8];
+        __shared__ float red[kBlockThreads / 32];
         if (TPR == 32) {
             if (lane == 0) red[group] = total;
             __syncthreads();
@@ -366,173 +420,163 @@ __global__ void __launch_bounds__(TPR == 32 ? 256 : 512) logprob_rows_kernel(LpA
 }
 
 // ---- maps -------------------------------------------------------------------------------------------------------
-// Tiles as in norm.cu: lp lanes of V pixels each, channels shared out to groups, CPT of them in a thread's registers (0: any number,
-// read again for each pass).  TOP: the best classes, found one after the other.
-template <class T, int V, int CPT, int MODE, bool TOP>
-__global__ void __launch_bounds__(256) logprob_map_kernel(LpArgs a, int lp, int tiles)
+// As in norm.cu: a lane has V pixels (4 bytes of them, or one value), `share` warps split the classes, up to CPT of them to a warp, in
+// registers.  CPT = 0: any number, read again for every pass.  If share is 1 the warps of a block take a tile each and need no barrier.
+constexpr int kMapWarps = 16;
+
+// Best of each pixel over the warps of the block; `red`: a value a thread, not read or written by others until the next barrier.
+template <class V, class F> __device__ __forceinline__ V across_warps(V v, int share, V* red, F better)
 {
-    constexpr int kWarps = 8;
-    __shared__ float red[2][kWarps * 32 * V];
-    __shared__ unsigned long long round[2][TOP ? kWarps * 32 : 1];
+    if (share == 1) return v;
+    const int lane = threadIdx.x & 31;
+    red[threadIdx.x] = v;
+    __syncthreads();
+    v = red[lane];
+    for (int w = 1; w < share; ++w) v = better(v, red[w * 32 + lane]);
+    return v;
+}
+
+template <class T, int V, int CPT, int MODE, bool TOP, bool FULL>
+__device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int px, int first, int per, int share, float over, float& total,
+                                             float (*red)[32 * kMapWarps * V], unsigned long long (*keys)[TOP ? 32 * kMapWarps : 1])
+{
+    const int count = FULL ? CPT : min(per, a.c - first);
+    const bool live = FULL || px < a.p;
+    const long long row = n * a.p + px;
+    const T* zt = static_cast<const T*>(a.z) + n * a.z_stride + px;
+    const unsigned bytes = (unsigned)a.p * sizeof(T);
+    const char* base = reinterpret_cast<const char*>(zt + (long long)first * a.p);
+    auto load = [&](int i) {
+        Pack<T, V> r = filled<T, V>(from_f<T>(minus_inf()));
+        if (live && i < count) r = load_pack<T, V>(reinterpret_cast<const T*>(base + (unsigned long long)bytes * (unsigned)i));
+        return r;
+    };
+    Pack<T, V> raw[CPT ? CPT : 1];
+    if constexpr (CPT > 0) {
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) raw[i] = load(i);
+    }
+    Label label[V];
+    if (live && (MODE == kLoss || first == 0)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) label[j] = read_label<T>(a, row + j, zt + j, a.p);
+    }
+    auto each = [&](auto f) {
+        if constexpr (CPT > 0) {
+#pragma unroll
+            for (int i = 0; i < CPT; ++i)
+                if (i < count) f(raw[i], i);
+        } else
+            for (int i = 0; i < count; ++i) f(load(i), i);
+    };
+    Vals<V> m = all<V>(minus_inf()), s = all<V>(0.f), t = all<V>(0.f);
+    each([&](const Pack<T, V>& r, int) {
+        const Vals<V> z = values(r);
+#pragma unroll
+        for (int j = 0; j < V; ++j) m.v[j] = fmaxf(m.v[j], z.v[j]);
+    });
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        m.v[j] = across_warps(m.v[j], share, red[0] + j * 32 * kMapWarps, [](float x, float y) { return fmaxf(x, y); });
+        if (m.v[j] == minus_inf()) m.v[j] = 0.f;
+    }
+    const Vals<V> minus_m = mul(m, all<V>(-1.f));
+    each([&](const Pack<T, V>& r, int) {
+        Vals<V> x = mul(add(values(r), minus_m), all<V>(kLog2e)), e;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (MODE == kStats) x.v[j] = max_nan(x.v[j], kLeast);
+            e.v[j] = ex2(x.v[j]);
+        }
+        s = add(s, e);
+        if (MODE == kStats) t = fma(e, x, t);
+    });
+    // (three buffers in turn: each is written again only after a barrier that follows its last reading)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        s.v[j] = across_warps(s.v[j], share, red[1] + j * 32 * kMapWarps, [](float x, float y) { return x + y; });
+        if (MODE == kStats) t.v[j] = across_warps(t.v[j], share, red[2] + j * 32 * kMapWarps, [](float x, float y) { return x + y; });
+    }
+    RowResult r[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) r[j] = result_of(Sums{m.v[j], s.v[j], t.v[j]});
+    if (MODE == kStats && live && first == 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) write_stats(a, row + j, r[j], label[j]);
+    }
+    if constexpr (TOP) {
+        unsigned long long before = ~0ull;
+        for (int k = 0; k < a.top; ++k) {
+            unsigned long long best = 0;
+            each([&](const Pack<T, V>& q, int i) {
+                const unsigned long long key = key_of(to_f(q.v[0]), first + i);
+                if (key < before && key > best) best = key;
+            });
+            before = across_warps(best, share, keys[k & 1], [](unsigned long long x, unsigned long long y) { return x > y ? x : y; });
+            if (live && first == 0) {
+                const long long at = (n * a.top + k) * a.p + px;
+                if (a.top_logp) a.top_logp[at] = logp_of(r[0], value_of(before));
+                if (a.top_index) a.top_index[at] = class_of(before);
+            }
+        }
+    }
+    if (MODE == kLoss) {
+        Vals<V> g, f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (!live) { f.v[j] = g.v[j] = 0.f; continue; }
+            f.v[j] = label[j].has > 0 ? (r[j].empty ? 0.f : over) : label[j].has == 0 ? 0.f : nan_f();
+            g.v[j] = f.v[j] == 0.f ? 0.f : f.v[j] / s.v[j];
+            if (first == 0 && label[j].has) total += logp_of_label(r[j], label[j]);
+        }
+        if (a.dz && live) {
+            char* out = reinterpret_cast<char*>(static_cast<T*>(a.dz) + n * a.dz_stride + (long long)first * a.p + px);
+            each([&](const Pack<T, V>& q, int i) {
+                Vals<V> x = mul(add(values(q), minus_m), all<V>(kLog2e));
+#pragma unroll
+                for (int j = 0; j < V; ++j) x.v[j] = ex2(x.v[j]);
+                x = mul(x, g);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    if (f.v[j] == 0.f) x.v[j] = 0.f;            // (whatever the logits are)
+                    if (first + i == (int)label[j].cls) x.v[j] -= f.v[j];
+                }
+                store_pack<T, V>(reinterpret_cast<T*>(out + (unsigned long long)bytes * (unsigned)i), rounded<T, V>(x));
+            });
+        }
+    }
+}
+
+template <class T, int V, int CPT, int MODE, bool TOP>
+__global__ void __launch_bounds__(32 * kMapWarps) logprob_map_kernel(LpArgs a, int share, int per, int tiles)
+{
+    __shared__ float red[3][32 * kMapWarps * V];
+    __shared__ unsigned long long keys[2][TOP ? 32 * kMapWarps : 1];
     previous_launches();
-    const int l = threadIdx.x & (lp - 1), g = threadIdx.x / lp, groups = blockDim.x / lp, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int slots = CPT ? CPT : (a.c + groups - 1) / groups;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, groups = warps / share;
+    const int first = (warp & (share - 1)) * per;
     float over = 0.f, total = 0.f;
     if (MODE == kLoss) {
         const float k = labelled_rows(a);
         over = k > 0.f ? a.scale / k : 0.f;
     }
-    for (long long tile = blockIdx.x; tile < a.n * tiles; tile += gridDim.x) {
+    for (long long tile = (long long)blockIdx.x * groups + warp / share; tile < a.n * tiles; tile += (long long)gridDim.x * groups) {
         const long long n = tile / tiles;
-        const int px = (int)(tile - n * tiles) * lp * V + l * V;
-        const bool live = px < a.p;
-        const long long row = n * a.p + px;
-        const T* zt = static_cast<const T*>(a.z) + n * a.z_stride + px;
-        auto load = [&](int i) {
-            const int ch = g + i * groups;
-            if (live && ch < a.c) return load_pack<T, V>(zt + (long long)ch * a.p);
-            Pack<T, V> r;
-#pragma unroll
-            for (int j = 0; j < V; ++j) r.v[j] = from_f<T>(minus_inf());
-            return r;
-        };
-        Pack<T, V> raw[CPT ? CPT : 1];
-        if constexpr (CPT > 0) {
-#pragma unroll
-            for (int i = 0; i < CPT; ++i) raw[i] = load(i);
-        }
-        Label label[V];
-        if (live && (MODE == kLoss || g == 0)) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) label[j] = read_label<T>(a, row + j, zt + j, a.p);
-        }
-        auto each = [&](auto f) {
-            if constexpr (CPT > 0) {
-#pragma unroll
-                for (int i = 0; i < CPT; ++i) f(raw[i], i);
-            } else
-                for (int i = 0; i < slots; ++i) f(load(i), i);
-        };
-        float m[V], s[V], t[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) { m[j] = minus_inf(); s[j] = t[j] = 0.f; }
-        each([&](const Pack<T, V>& r, int) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) m[j] = fmaxf(m[j], to_f(r.v[j]));
-        });
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            for (int d = 16; d >= lp; d >>= 1) m[j] = fmaxf(m[j], __shfl_xor_sync(0xffffffffu, m[j], d));
-        if (lane < lp) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) red[0][(warp * V + j) * lp + lane] = m[j];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            m[j] = minus_inf();
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) m[j] = fmaxf(m[j], red[0][(w * V + j) * lp + (lane & (lp - 1))]);
-            if (m[j] == minus_inf()) m[j] = 0.f;
-        }
-        each([&](const Pack<T, V>& r, int) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float x = max_nan(exponent_of(to_f(r.v[j]), m[j]), kLeast), e = ex2(x);
-                s[j] += e;
-                if (MODE == kStats) t[j] = fmaf(e, x, t[j]);
-            }
-        });
-        // sums over the channels; the second buffer, then the first again, which all threads have read by the barrier in between
-        auto sum_up = [&](float (&v)[V], float* buffer) {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                for (int d = 16; d >= lp; d >>= 1) v[j] += __shfl_xor_sync(0xffffffffu, v[j], d);
-            if (lane < lp) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) buffer[(warp * V + j) * lp + lane] = v[j];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                v[j] = 0.f;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) v[j] += buffer[(w * V + j) * lp + (lane & (lp - 1))];
-            }
-        };
-        sum_up(s, red[1]);
-        if (MODE == kStats) sum_up(t, red[0]);
-        RowResult r[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) r[j] = result_of(Sums{m[j], s[j], t[j]});
-        if (MODE == kStats && live && g == 0) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) write_stats(a, row + j, r[j], label[j]);
-        }
-        if constexpr (TOP) {
-            unsigned long long before = ~0ull;
-            for (int k = 0; k < a.top; ++k) {
-                unsigned long long mine = 0;
-                each([&](const Pack<T, V>& q, int i) {
-                    const int ch = g + i * groups;
-                    const unsigned long long key = ch < a.c ? key_of(to_f(q.v[0]), ch) : 0ull;
-                    if (key < before && key > mine) mine = key;
-                });
-                for (int d = 16; d >= lp; d >>= 1) {
-                    const unsigned long long u = __shfl_xor_sync(0xffffffffu, mine, d);
-                    if (u > mine) mine = u;
-                }
-                if (lane < lp) round[k & 1][warp * lp + lane] = mine;
-                __syncthreads();
-                mine = 0;
-#pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const unsigned long long u = round[k & 1][w * lp + (lane & (lp - 1))];
-                    if (u > mine) mine = u;
-                }
-                before = mine;
-                if (live && g == 0) {
-                    const long long at = (n * a.top + k) * a.p + px;
-                    if (a.top_logp) a.top_logp[at] = logp_of(r[0], value_of(mine));
-                    if (a.top_index) a.top_index[at] = class_of(mine);
-                }
-            }
-        }
-        if (MODE == kLoss) {
-            float f[V], gr[V];
-            if (live) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    f[j] = label[j].has > 0 ? (r[j].empty ? 0.f : over) : label[j].has == 0 ? 0.f : nan_f();
-                    gr[j] = f[j] / s[j];
-                    if (g == 0 && label[j].has) total += logp_of_label(r[j], label[j]);
-                }
-                if (a.dz) {
-                    T* dt = static_cast<T*>(a.dz) + n * a.dz_stride + px;
-                    each([&](const Pack<T, V>& q, int i) {
-                        const int ch = g + i * groups;
-                        if (ch >= a.c) return;
-                        Pack<T, V> d;
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const float x = ex2(exponent_of(to_f(q.v[j]), m[j])) * gr[j];
-                            d.v[j] = from_f<T>(f[j] == 0.f ? 0.f : ch == label[j].cls ? x - f[j] : x);
-                        }
-                        store_pack<T, V>(dt + (long long)ch * a.p, d);
-                    });
-                }
-            }
-        }
-        __syncthreads();
+        const int px0 = (int)(tile - n * tiles) * 32 * V;
+        if (CPT > 0 && first + CPT <= a.c && per == CPT && px0 + 32 * V <= a.p)
+            logprob_tile<T, V, CPT, MODE, TOP, (CPT > 0)>(a, n, px0 + lane * V, first, per, share, over, total, red, keys);
+        else
+            logprob_tile<T, V, CPT, MODE, TOP, false>(a, n, px0 + lane * V, first, per, share, over, total, red, keys);
+        if (TOP && share > 1) __syncthreads();                  // (the keys' two buffers start over)
     }
     if (MODE == kLoss && a.sums) {
-        total = lanes_sum(total, 32);
+        total = lanes_sum(total);
         __syncthreads();
         if (lane == 0) red[0][warp] = total;
         __syncthreads();
         if (threadIdx.x == 0) {
             float sum = 0.f;
-            for (int w = 0; w < kWarps; ++w) sum += red[0][w];
+            for (int w = 0; w < warps; ++w) sum += red[0][w];
             a.sums[blockIdx.x] = sum;
         }
     }
@@ -574,25 +618,29 @@ __global__ void __launch_bounds__(512) loss_finish_kernel(LpArgs a, int sums, fl
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
-// What a row's classes share: dlogits = w_l (class = label) - p (w_l + w_h (log p + entropy)).
-struct RowGrad { float lse, wl, wh, h; long long cls; bool empty; };
+// What a row's classes share: dlogits = w_l (class = label) - p (w_l + w_h (log p + entropy)) = w_l (class = label) - p (base + slope x)
+// with x = log2 p.
+struct RowGrad { float lse, wl, base, slope; int cls; };
 __device__ __forceinline__ RowGrad row_grad(const LpArgs& a, long long row)
 {
     RowGrad r;
     r.lse = a.lse_in[row];
-    r.cls = a.labels ? a.labels[row] : -1;
+    const long long cls = a.labels ? a.labels[row] : -1;
+    r.cls = cls >= 0 && cls < a.c ? (int)cls : -1;
     r.wl = a.dlogp && r.cls >= 0 ? a.dlogp[row] : 0.f;
-    if (r.cls >= a.c) r.wl = nan_f();
-    r.wh = a.dentropy ? a.dentropy[row] : 0.f;
-    r.h = a.dentropy ? a.entropy_in[row] : 0.f;
-    r.empty = r.lse == minus_inf();
+    if (cls >= a.c) r.wl = nan_f();
+    const float wh = a.dentropy ? a.dentropy[row] : 0.f;
+    r.base = a.dentropy ? fmaf(wh, a.entropy_in[row], r.wl) : r.wl;
+    r.slope = wh * kLn2;
+    if (r.lse == minus_inf()) { r.lse = INFINITY; r.wl = r.base = r.slope = 0.f; }         // nothing left: all p are 0
     return r;
 }
-__device__ __forceinline__ float class_grad(const RowGrad& r, float z, bool hit)
+template <int V> __device__ __forceinline__ Vals<V> class_grads(const Vals<V>& z, const Vals<V>& minus_lse, const Vals<V>& slope, const Vals<V>& base)
 {
-    const float lp = max_nan(z - r.lse, -110.f), p = ex2(lp * kLog2e);       // e^-110 is 0 in fp32
-    const float d = (hit ? r.wl : 0.f) - p * fmaf(r.wh, lp + r.h, r.wl);
-    return r.empty ? 0.f : d;
+    Vals<V> x = mul(add(z, minus_lse), all<V>(kLog2e)), p;
+#pragma unroll
+    for (int j = 0; j < V; ++j) { x.v[j] = max_nan(x.v[j], kLeast); p.v[j] = ex2(x.v[j]); }
+    return mul(mul(p, all<V>(-1.f)), fma(slope, x, base));
 }
 
 template <class T, int V, bool SHIFT> __global__ void __launch_bounds__(256) logprob_bwd_rows_kernel(LpArgs a, int segments)
@@ -610,17 +658,27 @@ template <class T, int V, bool SHIFT> __global__ void __launch_bounds__(256) log
         T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
         Pack<T, V> raw[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) raw[i] = load_logits<T, V>(zr, first + i * 32 * V, o, hi);
+        for (int i = 0; i < kPer; ++i) {
+            raw[i] = zero_pack<T, V>();
+            load_whole<T, V>(raw[i], zr, first + i * 32 * V, o, hi);
+        }
         const RowGrad r = row_grad(a, row);
-        const long long at = r.cls + o;
+        if (SHIFT || a.c % V) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) load_rest<T, V>(raw[i], zr, first + i * 32 * V, o, hi);
+        }
+        const int at = r.cls >= 0 ? r.cls + o : -1;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int e = first + i * 32 * V;
             if (e >= hi) continue;
-            Pack<T, V> d;
+            Vals<V> d = class_grads(values(raw[i]), all<V>(-r.lse), all<V>(r.slope), all<V>(r.base));
+            if ((unsigned)(at - e) < (unsigned)V && at >= 0) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) d.v[j] = from_f<T>(class_grad(r, to_f(raw[i].v[j]), r.cls >= 0 && e + j == at));
-            store_part<T, V>(dr, e, o, hi, d);
+                for (int j = 0; j < V; ++j)
+                    if (e + j == at) d.v[j] += r.wl;
+            }
+            store_part<T, V>(dr, e, o, hi, rounded<T, V>(d));
         }
     }
 }
@@ -628,7 +686,7 @@ template <class T, int V, bool SHIFT> __global__ void __launch_bounds__(256) log
 template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map_kernel(LpArgs a, int tiles, int slabs)
 {
     previous_launches();
-    constexpr int kSlab = 16, kAhead = 4;
+    constexpr int kSlab = 16, kAhead = 8;
     const int lane = threadIdx.x & 31;
     for (long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); task < a.n * tiles * slabs; task += (long long)gridDim.x * 8) {
         const long long at = task / slabs, n = at / tiles;
@@ -637,9 +695,13 @@ template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map
         if (px >= a.p) continue;
         const T* zt = static_cast<const T*>(a.z) + n * a.z_stride + px;
         T* dt = static_cast<T*>(a.dz) + n * a.dz_stride + px;
-        RowGrad r[V];
+        Vals<V> minus_lse, slope, base, wl;
+        int cls[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) r[j] = row_grad(a, n * a.p + px + j);
+        for (int j = 0; j < V; ++j) {
+            const RowGrad r = row_grad(a, n * a.p + px + j);
+            minus_lse.v[j] = -r.lse; slope.v[j] = r.slope; base.v[j] = r.base; wl.v[j] = r.wl; cls[j] = r.cls;
+        }
         for (int ch = c0; ch < c1; ch += kAhead) {
             Pack<T, V> raw[kAhead];
 #pragma unroll
@@ -648,10 +710,11 @@ template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (ch + i >= c1) continue;
-                Pack<T, V> d;
+                Vals<V> d = class_grads(values(raw[i]), minus_lse, slope, base);
 #pragma unroll
-                for (int j = 0; j < V; ++j) d.v[j] = from_f<T>(class_grad(r[j], to_f(raw[i].v[j]), ch + i == r[j].cls));
-                store_pack<T, V>(dt + (long long)(ch + i) * a.p, d);
+                for (int j = 0; j < V; ++j)
+                    if (ch + i == cls[j]) d.v[j] += wl.v[j];
+                store_pack<T, V>(dt + (long long)(ch + i) * a.p, rounded<T, V>(d));
             }
         }
     }
@@ -664,8 +727,9 @@ constexpr int kMostCounts = 1024;
 template <class T, int V, int NV, int TPR, bool SHIFT, int MODE> int run_rows(const LpArgs& a, int cluster, int part, int* blocks, cudaStream_t st)
 {
     auto kernel = logprob_rows_kernel<T, V, NV, TPR, SHIFT, MODE>;
-    const int threads = TPR == 32 ? 256 : 512, per = TPR == 32 ? 8 : 1;
-    const long long want = (a.rows + per - 1) / per, most = (TPR == 32 ? kMostBlocks : 4 * kSms) / cluster;
+    const int threads = kBlockThreads, per = kBlockThreads / TPR;
+    const int fit = resident<logprob_rows_kernel<T, V, NV, TPR, SHIFT, MODE>>(threads, 0);
+    const long long want = (a.rows + per - 1) / per, most = (long long)kSms * (fit < 8 ? fit : 8) / cluster;
     *blocks = (int)(want < most ? want : most) * cluster;
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -685,16 +749,15 @@ template <class T, int V, int NV, int TPR, bool SHIFT, int MODE> int run_rows(co
 template <class T, int V, bool SHIFT, int MODE> int pick_rows(const LpArgs& a, int* blocks, cudaStream_t st)
 {
     const int vecs = (a.c + (SHIFT ? V - 1 : 0) + V - 1) / V;
-    constexpr int kSmall = 8 / V ? 8 / V : 1, kMid = V == 8 ? 4 : 32 / V, kWide = V == 8 ? 8 : 32 / V;
+    constexpr int kSmall = 8 / V ? 8 / V : 1, kMid = V == 1 ? 32 : 8, kPart = V == 1 ? 16 : 4, kWide = V == 1 ? 64 : 16;
     if (vecs <= 32 * kSmall) return run_rows<T, V, kSmall, 32, SHIFT, MODE>(a, 1, vecs * V, blocks, st);
     if (vecs <= 32 * kMid) return run_rows<T, V, kMid, 32, SHIFT, MODE>(a, 1, vecs * V, blocks, st);
     int cluster = 1;
     auto share = [&] { return (vecs + cluster - 1) / cluster; };
-    while (share() > 512 * kWide) cluster *= 2;
-    while (cluster < 16 && a.rows * cluster * 2 <= 2 * kSms && share() > 512 * kSmall) cluster *= 2;
-    if (share() <= 512 * kSmall) return run_rows<T, V, kSmall, 512, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
-    if (share() <= 512 * kMid) return run_rows<T, V, kMid, 512, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
-    return run_rows<T, V, kWide, 512, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
+    while (share() > kBlockThreads * kWide) cluster *= 2;
+    while (cluster < 16 && a.rows * cluster * 2 <= 2 * kSms && share() > kBlockThreads * kPart) cluster *= 2;
+    if (share() <= kBlockThreads * kPart) return run_rows<T, V, kPart, kBlockThreads, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
+    return run_rows<T, V, kWide, kBlockThreads, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
 }
 
 template <class T, int MODE> int rows(const LpArgs& a, int* blocks, cudaStream_t st)
@@ -708,27 +771,32 @@ template <class T, int MODE> int rows(const LpArgs& a, int* blocks, cudaStream_t
     return pick_rows<T, 1, false, MODE>(a, blocks, st);
 }
 
+// Warps that share a tile's classes, and classes of each: the fewest warps of up to 32 classes; 16 warps and any number of classes beyond.
 template <class T, int V, int MODE, bool TOP> int run_map(const LpArgs& a, int* blocks, cudaStream_t st)
 {
-    int lp = 32;
-    auto per = [&] { return (a.c + 256 / lp - 1) / (256 / lp); };
-    while (per() > 4 && lp * V > 32) lp >>= 1;
-    const long long tiles = (a.p + lp * V - 1) / (lp * V), all = a.n * tiles;
+    const long long tiles = (a.p + 32 * V - 1) / (32 * V), all = a.n * tiles;
+    int share = 1;
+    while (share < kMapWarps && (a.c + share - 1) / share > 32) share *= 2;
+    const int per = (a.c + share - 1) / share, warps = share > 1 ? share : 4, groups = warps / share;
     const LaunchStream ls{st, true};
-    auto go = [&](auto kernel, int per_sm) {
-        const long long most = (long long)kSms * per_sm;
-        *blocks = (int)(all < most ? all : most);
-        launch(kernel, dim3(*blocks), dim3(256), 0, ls, a, lp, (int)tiles);
-        return launched();
-    };
-    if (per() <= 1) return go(logprob_map_kernel<T, V, 1, MODE, TOP>, 8);
-    if (per() <= 4) return go(logprob_map_kernel<T, V, 4, MODE, TOP>, 4);
-    if (per() <= 16) return go(logprob_map_kernel<T, V, 16, MODE, TOP>, 2);
-    return go(logprob_map_kernel<T, V, 0, MODE, TOP>, 4);
+#define GO(...)                                                                                                                              \
+    do {                                                                                                                                     \
+        const int fit = resident<__VA_ARGS__>(warps * 32, 0);                                                                                \
+        const long long want = (all + groups - 1) / groups, most = (long long)kSms * (fit < 8 ? fit : 8);                                    \
+        *blocks = (int)(want < most ? want : most);                                                                                          \
+        launch(__VA_ARGS__, dim3(*blocks), dim3(warps * 32), 0, ls, a, share, per, (int)tiles);                                              \
+        return launched();                                                                                                                   \
+    } while (0)
+    if (per <= 8) GO(logprob_map_kernel<T, V, 8, MODE, TOP>);
+    if (per <= 24) GO(logprob_map_kernel<T, V, 24, MODE, TOP>);
+    if (per <= 32) GO(logprob_map_kernel<T, V, 32, MODE, TOP>);
+    GO(logprob_map_kernel<T, V, 0, MODE, TOP>);
+#undef GO
 }
 
 template <class T> bool map_vector(const LpArgs& a, int v)
 {
+    if (v == 1) return true;
     auto fits = [&](const void* p, long long stride) { return !p || (aligned(p, v * sizeof(T)) && (a.n == 1 || stride % v == 0)); };
     return a.p % v == 0 && fits(a.z, a.z_stride) && fits(a.dz, a.dz_stride);
 }
@@ -738,7 +806,7 @@ template <class T, int MODE> int forward(const LpArgs& a, int* blocks, cudaStrea
     if (a.p == 1) return rows<T, MODE>(a, blocks, st);
     if constexpr (MODE == kStats)
         if (a.top > 0) return run_map<T, 1, MODE, true>(a, blocks, st);
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 4 / sizeof(T);
     if (map_vector<T>(a, V)) return run_map<T, V, MODE, false>(a, blocks, st);
     return run_map<T, 1, MODE, false>(a, blocks, st);
 }

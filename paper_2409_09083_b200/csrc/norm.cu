@@ -122,7 +122,12 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
             raw[i] = zero_pack<T, V>();
-            if (e < hi) raw[i] = kWhole ? load_pack<T, V>(xr + i * tpr * V) : load_part<T, V>(xr - t * V, e, o, hi);
+            if (kWhole) { if (e < hi) raw[i] = load_pack<T, V>(xr + i * tpr * V); }
+            else load_whole<T, V>(raw[i], xr - t * V, e, o, hi);
+        }
+        if (!kWhole) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) load_rest<T, V>(raw[i], xr - t * V, (i * tpr + t) * V, o, hi);
         }
         Vals<V> acc = values(raw[0]);
 #pragma unroll
@@ -184,7 +189,8 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
             for (int i = 0; i < VPT; ++i) {
                 const int skip = i * tpr * V, e = skip + t * V;
                 Pack<T, V> again = zero_pack<T, V>();
-                if (e < hi) again = load_part<T, V>(xr - t * V, e, 0, hi);
+                load_whole<T, V>(again, xr - t * V, e, 0, hi);
+                load_rest<T, V>(again, xr - t * V, e, 0, hi);
                 const Vals<V> v = values(again);
                 if (!special<T>(largest(v))) continue;
                 unsigned ex;
@@ -262,11 +268,23 @@ __device__ __forceinline__ void load_row(const RowAt<T>& at, bool live, int c, i
         in.dy[i] = zero_pack<T, V>();
         in.x[i].clear();
         if (live && e < c) {
-            in.dy[i] = kWhole ? load_pack<T, V>(at.dy + skip) : load_part<T, V>(at.dy - t * V, e, 0, c);
+            if (kWhole) in.dy[i] = load_pack<T, V>(at.dy + skip);
+            else load_whole<T, V>(in.dy[i], at.dy - t * V, e, 0, c);
             if constexpr (CK) {
                 in.x[i].q = load_pack<unsigned char, V>(at.q + skip);
                 in.x[i].e = at.e[skip / kBlock];
-            } else in.x[i].a = kWhole ? load_pack<T, V>(at.x + skip) : load_part<T, V>(at.x - t * V, e, 0, c);
+            } else {
+                if (kWhole) in.x[i].a = load_pack<T, V>(at.x + skip);
+                else load_whole<T, V>(in.x[i].a, at.x - t * V, e, 0, c);
+            }
+        }
+    }
+    if (!kWhole && live) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int e = (i * tpr + t) * V;
+            load_rest<T, V>(in.dy[i], at.dy - t * V, e, 0, c);
+            if constexpr (!CK) load_rest<T, V>(in.x[i].a, at.x - t * V, e, 0, c);
         }
     }
 }
