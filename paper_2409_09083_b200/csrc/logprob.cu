@@ -23,7 +23,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -160.f;                       // 2^-160 is 0 in fp32: where a = -inf would make 0 * inf
 constexpr int kTop = FTP_TOP_MAX;
 constexpr int kParts = 32;                             // parts of a row, whose maxima bound its best values
-constexpr int kBlockThreads = 256;
+constexpr int kBlockThreads = 512;
 constexpr int kListBlock = 512, kListWarp = 64;        // candidates
 constexpr int kCountHere = 4096;                       // rows whose labels every block counts by itself
 
@@ -182,24 +182,10 @@ __device__ __forceinline__ float bound_of(float v, int top)
     return __uint_as_float(best & 0x80000000u ? best & 0x7fffffffu : ~best);
 }
 
-// A group of TPR threads (a warp, or the block) holds a row, or with a cluster its part of one, as NV vectors of V logits a
-// thread.  SHIFT as in norm.cu: vectors lie on the 16-byte grid below the row's start.
-template <int TPR> struct RowShared {
-    static constexpr int kGroups = TPR == 32 ? kBlockThreads / 32 : 1;
-    static constexpr int kList = TPR == 32 ? kListWarp : kListBlock;
-    unsigned long long list[kGroups][kList];
-    unsigned long long best[kTop];           // a block's own best, for the cluster
-    unsigned long long round[32];
-    float parts[kParts];
-    Sums sums[2][32];                        // of the warps; of this row and the one before
-    int count[2][kGroups];
-    Sums whole;
-};
-
-// The `top` best of `m` keys in `list`, by counting; write(place, key) for each.
-template <int TPR, class F> __device__ __forceinline__ void place(const unsigned long long* list, int m, int top, int t, F write)
+// The `top` best of `m` keys in `list`, found by `threads` threads by counting; write(place, key) for each.
+template <class F> __device__ __forceinline__ void place(const unsigned long long* list, int m, int top, int t, int threads, F write)
 {
-    for (int i = t; i < m; i += TPR) {
+    for (int i = t; i < m; i += threads) {
         const unsigned long long k = list[i];
         int better = 0;
         for (int j = 0; j < m; ++j) better += list[j] > k;
@@ -221,140 +207,293 @@ __device__ __forceinline__ Sums join_lanes(const Sums* of, int n)
     return s;
 }
 
-template <class T, int V, int NV, int TPR, bool SHIFT, int MODE>
-__global__ void __launch_bounds__(kBlockThreads, NV * sizeof(Pack<T, V>) > 128 && (sizeof(T) == 4 || V == 1) ? 1 : 2) logprob_rows_kernel(LpArgs a, int cluster, int part)
+// Adds a vector's exponents to the sums of a thread.
+template <int MODE, int V> __device__ __forceinline__ void take_sums(const Vals<V>& z, float shift, Vals<V>& s, Vals<V>& t)
 {
-    __shared__ RowShared<TPR> sh;
+    Vals<V> x = mul(add(z, all<V>(-shift)), all<V>(kLog2e)), e;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        if (MODE == kStats) x.v[j] = max_nan(x.v[j], kLeast);
+        e.v[j] = ex2(x.v[j]);
+    }
+    s = add(s, e);
+    if (MODE == kStats) t = fma(e, x, t);
+}
+
+// dlogits of a vector of places e ..: g 2^((z - m) log2 e), less f at the label's place `at`; 0 if f is.
+template <int V> __device__ __forceinline__ Vals<V> loss_grads(const Vals<V>& z, float m, float g, float f, int e, int at)
+{
+    Vals<V> x = mul(add(z, all<V>(-m)), all<V>(kLog2e));
+#pragma unroll
+    for (int j = 0; j < V; ++j) x.v[j] = ex2(x.v[j]);
+    x = mul(x, all<V>(g));
+    if (f == 0.f) x = all<V>(0.f);                              // (whatever the logits are)
+    if ((unsigned)(at - e) < (unsigned)V && at >= 0) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (e + j == at) x.v[j] -= f;
+    }
+    return x;
+}
+
+// Rows that a warp holds in its registers, as NV vectors of V logits a lane.  SHIFT as in norm.cu: vectors lie on the 16-byte grid below
+// the row's start.
+constexpr int kRowWarps = 8;
+
+template <class T, int V, int NV, bool SHIFT, int MODE>
+__global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(LpArgs a)
+{
+    __shared__ unsigned long long lists[kRowWarps][kListWarp];
+    __shared__ int counts[kRowWarps];
+    __shared__ float totals[kRowWarps];
     previous_launches();
-    constexpr int kGroups = RowShared<TPR>::kGroups, kWarps = TPR / 32;
-    const int t = threadIdx.x & (TPR - 1), group = threadIdx.x / TPR, lane = threadIdx.x & 31;
-    const int rank = TPR == 32 ? 0 : (int)(blockIdx.x % cluster);
-    const long long step = (long long)(gridDim.x / cluster) * kGroups;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long* list = lists[warp];
+    int* count = counts + warp;
     const bool want_top = MODE == kStats && a.top > 0;
     float over = 0.f, total = 0.f;
     if (MODE == kLoss) {
         const float k = labelled_rows(a);
         over = k > 0.f ? a.scale / k : 0.f;
     }
-    Pack<T, V> raw[NV];
-    auto load_row = [&](long long row) {
+    for (long long row = (long long)blockIdx.x * kRowWarps + warp; row < a.rows; row += (long long)gridDim.x * kRowWarps) {
         const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
-        const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0;
-        const int first = rank * part, last = min(o + a.c, first + part);
-        zr -= o;
+        const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0, last = o + a.c;
+        Pack<T, V> raw[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             raw[i] = filled<T, V>(from_f<T>(minus_inf()));
-            load_whole<T, V>(raw[i], zr, first + (i * TPR + t) * V, o, last);
+            load_whole<T, V>(raw[i], zr - o, (i * 32 + lane) * V, o, last);
         }
+        Label label{-1, 0.f, 0};
+        if (MODE == kLoss || lane == 0) label = read_label<T>(a, row, zr, 1);
         if (SHIFT || a.c % V) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) load_rest<T, V>(raw[i], zr, first + (i * TPR + t) * V, o, last);
+            for (int i = 0; i < NV; ++i) load_rest<T, V>(raw[i], zr - o, (i * 32 + lane) * V, o, last);
         }
-    };
-    long long row = (long long)(blockIdx.x / cluster) * kGroups + group;
-    if (row < a.rows) load_row(row);
-    if (threadIdx.x < 2 * kGroups) sh.count[threadIdx.x / kGroups][threadIdx.x % kGroups] = 0;
-    __syncthreads();
-    int turn = 0;
-    for (; row < a.rows; row += step, turn ^= 1) {              // (a warp's own rows, or the whole block's or cluster's)
-        const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
-        const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0;
-        const int first = rank * part, last = min(o + a.c, first + part);
-        Label label{-1, 0.f, 0};
-        if (MODE == kLoss || t == 0) label = read_label<T>(a, row, zr, 1);
         Largest<T, V> most;
 #pragma unroll
         for (int i = 0; i < NV; ++i) most.take(raw[i]);
-        const float mine = most.value();
-        // largest of a part of the row, and of the warp, which the exponents are taken from
-        constexpr int kLanes = TPR / kParts;                    // of a part
-        float part_max = lanes_max(mine, kLanes);
-        if (TPR != 32 && want_top && lane % kLanes == 0) sh.parts[t / kLanes] = part_max;
-        const float m = lanes_max(part_max), shift = m == minus_inf() ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) keep_packed(raw[i]);
+        const float mine = most.value(), m = lanes_max(mine), shift = m == minus_inf() ? 0.f : m;
         Vals<V> s = all<V>(0.f), x2 = all<V>(0.f);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            Vals<V> x = mul(add(values(raw[i]), all<V>(-shift)), all<V>(kLog2e)), e;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if (MODE == kStats) x.v[j] = max_nan(x.v[j], kLeast);
-                e.v[j] = ex2(x.v[j]);
-            }
-            s = add(s, e);
-            if (MODE == kStats) x2 = fma(e, x, x2);
-        }
+        for (int i = 0; i < NV; ++i) take_sums<MODE, V>(values(raw[i]), shift, s, x2);
         Sums sums{shift, lanes_sum(sum_of(s)), 0.f};
         if (MODE == kStats) sums.t = lanes_sum(sum_of(x2));
-        if (TPR != 32) {
-            if (lane == 0) sh.sums[turn][t >> 5] = sums;
-            __syncthreads();
-            if (t < 32 || MODE == kLoss || cluster > 1) sums = join_lanes(sh.sums[turn], kWarps);
-            part_max = sh.parts[lane];
-        }
-        if (t == 0) sh.count[turn ^ 1][group] = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) keep_packed(raw[i]);
-        // the best classes of this part
-        int found = 0;
+        const RowResult r = result_of(sums);
+        if (MODE == kStats && lane == 0) write_stats(a, row, r, label);
         if (want_top) {
-            const float bound = bound_of(part_max, a.top);
+            if (lane == 0) *count = 0;
+            __syncwarp();
+            const float bound = bound_of(mine, a.top);
             if (mine >= bound) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    Largest<T, V> here;
-                    here.take(raw[i]);
-                    if (here.value() < bound) continue;
-                    const int e = first + (i * TPR + t) * V;
+                    const int e = (i * 32 + lane) * V;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float v = fmaxf(to_f(raw[i].v[j]), minus_inf());
                         if (v >= bound && e + j >= o && e + j < last) {
-                            const int at = atomicAdd(&sh.count[turn][group], 1);
-                            if (at < RowShared<TPR>::kList) sh.list[group][at] = key_of(v, e + j - o);
+                            const int at = atomicAdd(count, 1);
+                            if (at < kListWarp) list[at] = key_of(v, e + j - o);
                         }
                     }
                 }
             }
-            if (TPR == 32) __syncwarp(); else __syncthreads();
-            found = sh.count[turn][group];
-            if (found > RowShared<TPR>::kList) {                  // too many equal ones: one place after the other
+            __syncwarp();
+            int found = *count;
+            if (found > kListWarp) {                              // too many equal ones: one place after the other
+                unsigned long long before = ~0ull;
+                for (int k = 0; k < a.top; ++k) {
+                    unsigned long long best = 0;
+                    for (int e = lane; e < a.c; e += 32) {
+                        const unsigned long long key = key_of(to_f(zr[e]), e);
+                        if (key < before && key > best) best = key;
+                    }
+                    before = lanes_best(best, 32);
+                    if (lane == 0) list[k] = before;
+                }
+                found = a.top;
+                __syncwarp();
+            }
+            place(list, found, a.top, lane, 32, [&](int at, unsigned long long k) {
+                if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
+                if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
+            });
+            __syncwarp();
+        }
+        if (MODE == kLoss) {
+            if (lane == 0 && label.has) total += logp_of_label(r, label);
+            if (a.dz) {
+                T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
+                const float f = label.has > 0 ? (r.empty ? 0.f : over) : label.has == 0 ? 0.f : nan_f(), g = f == 0.f ? 0.f : f / sums.s;
+                const int at = label.has > 0 ? (int)label.cls + o : -1;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int e = (i * 32 + lane) * V;
+                    if (e < last) store_part<T, V>(dr, e, o, last, rounded<T, V>(loss_grads(values(raw[i]), sums.m, g, f, e, at)));
+                }
+            }
+        }
+    }
+    if (MODE == kLoss && a.sums) {
+        if (lane == 0) totals[warp] = total;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float s = 0.f;
+            for (int i = 0; i < kRowWarps; ++i) s += totals[i];
+            a.sums[blockIdx.x] = s;
+        }
+    }
+}
+
+// Longer rows: a block of 512 threads has a row, or with a cluster its part of one, in shared memory, and the next ones are on their way
+// into the other stages.  A thread copies (cp.async, 16 bytes each) what it will read itself, every 512th vector, so that no barrier
+// stands between copy and use, and the passes over the row are short loops: with the row in registers instead they had to be unrolled
+// in full and waited for instructions more than for anything else (4096 x 32000 bf16 with the eight best: 159 us).
+constexpr int kStageMost = 64 * 1024;            // bytes of a part: 32768 classes of 16 bits, 16384 of 32
+constexpr int kRingBytes = 200 * 1024;
+
+struct BlockShared {
+    unsigned long long list[kListBlock];
+    unsigned long long best[kTop];               // a block's own best, for the cluster
+    unsigned long long round[32];
+    float parts[kParts];
+    Sums sums[2][32];                            // of the warps; of this row and the one before
+    int count[2];
+    Sums whole;
+};
+
+__device__ __forceinline__ void copy_16(void* to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_of_row_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until all but the last `left` rows' copies of this thread have arrived.
+__device__ __forceinline__ void wait_rows(int left)
+{
+    if (left <= 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    else if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 2;" ::: "memory");
+}
+
+template <class T, bool SHIFT, int MODE>
+__global__ void __launch_bounds__(kBlockThreads, 1) logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_vec)
+{
+    constexpr int V = 16 / sizeof(T), kWarps = kBlockThreads / 32, kLanes = kBlockThreads / kParts;
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ BlockShared sh;
+    previous_launches();
+    const int t = threadIdx.x, lane = t & 31;
+    const int rank = (int)(blockIdx.x % cluster);
+    const long long step = gridDim.x / cluster;
+    const bool want_top = MODE == kStats && a.top > 0;
+    float over = 0.f, total = 0.f;
+    if (MODE == kLoss) {
+        const float k = labelled_rows(a);
+        over = k > 0.f ? a.scale / k : 0.f;
+    }
+    auto shift_of = [&](const T* zr) { return SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0; };
+    // places [first, last) of the row, on the grid that starts o below it, are this block's
+    auto fetch = [&](long long row, int stage) {
+        if (row < a.rows) {
+            const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
+            const int o = shift_of(zr), first = rank * part, last = min(o + a.c, first + part);
+            T* to = reinterpret_cast<T*>(ring + (size_t)stage * part * sizeof(T));
+            zr -= o;
+            for (int e = first + t * V; e < last; e += kBlockThreads * V) {
+                if (e >= o && e + V <= last) copy_16(to + (e - first), zr + e);
+                else {
+                    Pack<T, V> p = filled<T, V>(from_f<T>(minus_inf()));
+                    load_rest<T, V>(p, zr, e, o, last);
+                    store_pack<T, V>(to + (e - first), p);
+                }
+            }
+        }
+        copies_of_row_end();
+    };
+    long long row = blockIdx.x / cluster;
+    for (int i = 0; i + 1 < stages; ++i) fetch(row + i * step, i);
+    if (t < 2) sh.count[t] = 0;
+    __syncthreads();
+    int turn = 0, stage = 0;
+    for (; row < a.rows; row += step, turn ^= 1) {
+        const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
+        const int o = shift_of(zr), first = rank * part, last = min(o + a.c, first + part);
+        const T* mine_at = reinterpret_cast<const T*>(ring + (size_t)stage * part * sizeof(T)) + t * V;
+        const int count = last - first;                          // places from the part's start; a thread's are t V, t V + 512 V, ..
+        Label label{-1, 0.f, 0};
+        if (MODE == kLoss || t == 0) label = read_label<T>(a, row, zr, 1);
+        fetch(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+        wait_rows(stages - 1);
+        stage = stage + 1 == stages ? 0 : stage + 1;
+        Largest<T, V> most;
+#pragma unroll 4
+        for (int e = t * V, k = 0; e < count; e += kBlockThreads * V, ++k) most.take(load_pack<T, V>(mine_at + k * kBlockThreads * V));
+        const float mine = most.value();
+        // largest of a part of the row, and of the warp, which the exponents are taken from
+        float part_max = lanes_max(mine, kLanes);
+        if (want_top && lane % kLanes == 0) sh.parts[t / kLanes] = part_max;
+        const float m = lanes_max(part_max), shift = m == minus_inf() ? 0.f : m;
+        Vals<V> s = all<V>(0.f), x2 = all<V>(0.f);
+#pragma unroll 4
+        for (int e = t * V, k = 0; e < count; e += kBlockThreads * V, ++k)
+            take_sums<MODE, V>(values(load_pack<T, V>(mine_at + k * kBlockThreads * V)), shift, s, x2);
+        Sums sums{shift, lanes_sum(sum_of(s)), 0.f};
+        if (MODE == kStats) sums.t = lanes_sum(sum_of(x2));
+        if (lane == 0) sh.sums[turn][t >> 5] = sums;
+        __syncthreads();
+        if (t < 32 || MODE == kLoss || cluster > 1) sums = join_lanes(sh.sums[turn], kWarps);
+        if (t == 0) sh.count[turn ^ 1] = 0;
+        // the best classes of this part
+        int found = 0;
+        if (want_top) {
+            const float bound = bound_of(sh.parts[lane], a.top);
+            if (mine >= bound) {
+                for (int e = t * V, k = 0; e < count; e += kBlockThreads * V, ++k) {
+                    const Pack<T, V> p = load_pack<T, V>(mine_at + k * kBlockThreads * V);
+                    Largest<T, V> here;
+                    here.take(p);
+                    if (here.value() < bound) continue;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float v = fmaxf(to_f(p.v[j]), minus_inf());
+                        const int place = first + e + j;
+                        if (v >= bound && place >= o && place < last) {
+                            const int at = atomicAdd(&sh.count[turn], 1);
+                            if (at < kListBlock) sh.list[at] = key_of(v, place - o);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+            found = sh.count[turn];
+            if (found > kListBlock) {                             // too many equal ones: one place after the other
                 unsigned long long before = ~0ull;
                 const int places = min(a.top, found);
                 for (int k = 0; k < places; ++k) {
                     unsigned long long best = 0;
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) {
-                        const int e = first + (i * TPR + t) * V;
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const unsigned long long key = e + j >= o && e + j < last ? key_of(to_f(raw[i].v[j]), e + j - o) : 0ull;
-                            if (key < before && key > best) best = key;
-                        }
+                    for (int e = t; e < count; e += kBlockThreads) {
+                        const unsigned long long key = first + e >= o ? key_of(to_f(zr[first + e - o]), first + e - o) : 0ull;
+                        if (key < before && key > best) best = key;
                     }
                     best = lanes_best(best, 32);
-                    if (TPR != 32) {
-                        __syncthreads();
-                        if (lane == 0) sh.round[t >> 5] = best;
-                        __syncthreads();
-                        best = lanes_best(lane < kWarps ? sh.round[lane] : 0ull, 32);
-                    }
-                    before = best;
-                    if (t == 0) sh.list[group][k] = best;
+                    __syncthreads();
+                    if (lane == 0) sh.round[t >> 5] = best;
+                    __syncthreads();
+                    before = lanes_best(sh.round[lane & (kWarps - 1)], 32);
+                    if (t == 0) sh.list[k] = before;
                 }
                 found = places;
-                if (TPR == 32) __syncwarp(); else __syncthreads();
+                __syncthreads();
             }
         }
-        if (MODE == kStats && row + step < a.rows) load_row(row + step);       // on their way while this row's results are written
-        if (TPR != 32 && cluster > 1) {
+        if (cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (want_top) {
                 if (t < kTop) sh.best[t] = 0;
                 __syncthreads();
-                place<TPR>(sh.list[0], found, a.top, t, [&](int at, unsigned long long k) { sh.best[at] = k; });
+                place(sh.list, found, a.top, t, kBlockThreads, [&](int at, unsigned long long k) { sh.best[at] = k; });
             }
             if (t == 0) sh.whole = sums;
             cl.sync();
@@ -362,7 +501,7 @@ __global__ void __launch_bounds__(kBlockThreads, NV * sizeof(Pack<T, V>) > 128 &
             for (int r = 1; r < cluster; ++r) sums = join(sums, *cl.map_shared_rank(&sh.whole, r));
             if (want_top && rank == 0) {
                 found = cluster * a.top;
-                for (int i = t; i < found; i += TPR) sh.list[0][i] = cl.map_shared_rank(sh.best, i / a.top)[i % a.top];
+                for (int i = t; i < found; i += kBlockThreads) sh.list[i] = cl.map_shared_rank(sh.best, i / a.top)[i % a.top];
                 __syncthreads();
             }
         }
@@ -373,50 +512,31 @@ __global__ void __launch_bounds__(kBlockThreads, NV * sizeof(Pack<T, V>) > 128 &
                 if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
                 if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
             };
-            if (want_top && TPR != 32 && cluster > 1) place<TPR>(sh.list[0], found, a.top, t, best_of_row);
-            else if (want_top && t < 32) place<32>(sh.list[group], found, a.top, t, best_of_row);     // (this warp alone knows the row's sums)
+            if (want_top && cluster > 1) place(sh.list, found, a.top, t, kBlockThreads, best_of_row);
+            else if (want_top && t < 32) place(sh.list, found, a.top, t, 32, best_of_row);        // (this warp alone knows the row's sums)
         }
         if (MODE == kLoss) {
             if (t == 0 && rank == 0 && label.has) total += logp_of_label(r, label);
             if (a.dz) {
                 T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
-                const float f = label.has > 0 ? (r.empty ? 0.f : over) : label.has == 0 ? 0.f : nan_f();
-                const float g = f == 0.f ? 0.f : f / sums.s;
+                const float f = label.has > 0 ? (r.empty ? 0.f : over) : label.has == 0 ? 0.f : nan_f(), g = f == 0.f ? 0.f : f / sums.s;
                 const int at = label.has > 0 ? (int)label.cls + o : -1;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int e = first + (i * TPR + t) * V;
-                    if (e >= last) continue;
-                    Vals<V> x = mul(add(values(raw[i]), all<V>(-sums.m)), all<V>(kLog2e));
-#pragma unroll
-                    for (int j = 0; j < V; ++j) x.v[j] = ex2(x.v[j]);
-                    x = mul(x, all<V>(g));
-                    if (f == 0.f) x = all<V>(0.f);              // (whatever the logits are)
-                    if ((unsigned)(at - e) < (unsigned)V) {
+#pragma unroll 2
+                for (int k = 0, e = first + t * V; e < last; e += kBlockThreads * V, ++k) {
+                    const Pack<T, V> d = rounded<T, V>(loss_grads(values(load_pack<T, V>(mine_at + k * kBlockThreads * V)), sums.m, g, f, e, at));
+                    if (dz_vec) store_part<T, V>(dr, e, o, last, d);
+                    else {
 #pragma unroll
                         for (int j = 0; j < V; ++j)
-                            if (e + j == at) x.v[j] -= f;
+                            if (e + j >= o && e + j < last) dr[e + j] = d.v[j];
                     }
-                    store_part<T, V>(dr, e, o, last, rounded<T, V>(x));
                 }
             }
-            if (row + step < a.rows) load_row(row + step);
         }
-        if (TPR != 32 && cluster > 1) cg::this_cluster().sync();       // the others read this block's part
-        if (TPR == 32) __syncwarp();
+        if (cluster > 1) cg::this_cluster().sync();               // the others read this block's part
     }
-    if (MODE == kLoss && a.sums) {
-        __shared__ float red[kBlockThreads / 32];
-        if (TPR == 32) {
-            if (lane == 0) red[group] = total;
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                float s = 0.f;
-                for (int i = 0; i < kGroups; ++i) s += red[i];
-                a.sums[blockIdx.x] = s;
-            }
-        } else if (t == 0) a.sums[blockIdx.x] = total;
-    }
+    wait_rows(0);
+    if (MODE == kLoss && a.sums && t == 0) a.sums[blockIdx.x] = total;
 }
 
 // ---- maps -------------------------------------------------------------------------------------------------------
@@ -436,12 +556,12 @@ template <class V, class F> __device__ __forceinline__ V across_warps(V v, int s
     return v;
 }
 
-template <class T, int V, int CPT, int MODE, bool TOP, bool FULL>
+template <class T, int V, int CPT, int MODE, bool TOP>
 __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int px, int first, int per, int share, float over, float& total,
                                              float (*red)[32 * kMapWarps * V], unsigned long long (*keys)[TOP ? 32 * kMapWarps : 1])
 {
-    const int count = FULL ? CPT : min(per, a.c - first);
-    const bool live = FULL || px < a.p;
+    const int count = min(per, a.c - first);
+    const bool live = px < a.p;
     const long long row = n * a.p + px;
     const T* zt = static_cast<const T*>(a.z) + n * a.z_stride + px;
     const unsigned bytes = (unsigned)a.p * sizeof(T);
@@ -454,7 +574,20 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
     Pack<T, V> raw[CPT ? CPT : 1];
     if constexpr (CPT > 0) {
 #pragma unroll
-        for (int i = 0; i < CPT; ++i) raw[i] = load(i);
+        for (int i = 0; i < CPT; ++i) raw[i] = filled<T, V>(from_f<T>(minus_inf()));
+        if (live) {
+#pragma unroll
+            for (int i0 = 0; i0 < CPT; i0 += 8) {
+                if (i0 + 8 <= count) {
+#pragma unroll
+                    for (int i = i0; i < i0 + 8; ++i) raw[i] = load_pack<T, V>(reinterpret_cast<const T*>(base + (unsigned long long)bytes * (unsigned)i));
+                } else {
+#pragma unroll
+                    for (int i = i0; i < i0 + 8; ++i)
+                        if (i < count) raw[i] = load_pack<T, V>(reinterpret_cast<const T*>(base + (unsigned long long)bytes * (unsigned)i));
+                }
+            }
+        }
     }
     Label label[V];
     if (live && (MODE == kLoss || first == 0)) {
@@ -464,10 +597,22 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
     auto each = [&](auto f) {
         if constexpr (CPT > 0) {
 #pragma unroll
-            for (int i = 0; i < CPT; ++i)
-                if (i < count) f(raw[i], i);
-        } else
-            for (int i = 0; i < count; ++i) f(load(i), i);
+            for (int i0 = 0; i0 < CPT; i0 += 8) {               // eight without a test, where there are as many
+                if (i0 + 8 <= count) {
+#pragma unroll
+                    for (int i = i0; i < i0 + 8; ++i) f(raw[i], i);
+                } else {
+#pragma unroll
+                    for (int i = i0; i < i0 + 8; ++i)
+                        if (i < count) f(raw[i], i);
+                }
+            }
+        } else {
+            for (int i = 0; i < count; ++i) {
+                Pack<T, V> r = load(i);
+                f(r, i);
+            }
+        }
     };
     Vals<V> m = all<V>(minus_inf()), s = all<V>(0.f), t = all<V>(0.f);
     each([&](const Pack<T, V>& r, int) {
@@ -481,7 +626,8 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
         if (m.v[j] == minus_inf()) m.v[j] = 0.f;
     }
     const Vals<V> minus_m = mul(m, all<V>(-1.f));
-    each([&](const Pack<T, V>& r, int) {
+    constexpr bool kKeep = MODE == kLoss && CPT > 0 && sizeof(T) == 4;         // the exponentials take the logits' registers
+    each([&](Pack<T, V>& r, int) {
         Vals<V> x = mul(add(values(r), minus_m), all<V>(kLog2e)), e;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -490,6 +636,7 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
         }
         s = add(s, e);
         if (MODE == kStats) t = fma(e, x, t);
+        if (kKeep) r = rounded<T, V>(e);
     });
     // (three buffers in turn: each is written again only after a barrier that follows its last reading)
 #pragma unroll
@@ -532,9 +679,12 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
         if (a.dz && live) {
             char* out = reinterpret_cast<char*>(static_cast<T*>(a.dz) + n * a.dz_stride + (long long)first * a.p + px);
             each([&](const Pack<T, V>& q, int i) {
-                Vals<V> x = mul(add(values(q), minus_m), all<V>(kLog2e));
+                Vals<V> x = values(q);
+                if (!kKeep) {
+                    x = mul(add(x, minus_m), all<V>(kLog2e));
 #pragma unroll
-                for (int j = 0; j < V; ++j) x.v[j] = ex2(x.v[j]);
+                    for (int j = 0; j < V; ++j) x.v[j] = ex2(x.v[j]);
+                }
                 x = mul(x, g);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
@@ -563,10 +713,7 @@ __global__ void __launch_bounds__(32 * kMapWarps) logprob_map_kernel(LpArgs a, i
     for (long long tile = (long long)blockIdx.x * groups + warp / share; tile < a.n * tiles; tile += (long long)gridDim.x * groups) {
         const long long n = tile / tiles;
         const int px0 = (int)(tile - n * tiles) * 32 * V;
-        if (CPT > 0 && first + CPT <= a.c && per == CPT && px0 + 32 * V <= a.p)
-            logprob_tile<T, V, CPT, MODE, TOP, (CPT > 0)>(a, n, px0 + lane * V, first, per, share, over, total, red, keys);
-        else
-            logprob_tile<T, V, CPT, MODE, TOP, false>(a, n, px0 + lane * V, first, per, share, over, total, red, keys);
+        logprob_tile<T, V, CPT, MODE, TOP>(a, n, px0 + lane * V, first, per, share, over, total, red, keys);
         if (TOP && share > 1) __syncthreads();                  // (the keys' two buffers start over)
     }
     if (MODE == kLoss && a.sums) {
@@ -724,42 +871,50 @@ template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map
 constexpr int kMostBlocks = 8 * kSms;         // blocks of a loss, each with a sum
 constexpr int kMostCounts = 1024;
 
-template <class T, int V, int NV, int TPR, bool SHIFT, int MODE> int run_rows(const LpArgs& a, int cluster, int part, int* blocks, cudaStream_t st)
+template <class T, int V, int NV, bool SHIFT, int MODE> int run_warp_rows(const LpArgs& a, int* blocks, cudaStream_t st)
 {
-    auto kernel = logprob_rows_kernel<T, V, NV, TPR, SHIFT, MODE>;
-    const int threads = kBlockThreads, per = kBlockThreads / TPR;
-    const int fit = resident<logprob_rows_kernel<T, V, NV, TPR, SHIFT, MODE>>(threads, 0);
-    const long long want = (a.rows + per - 1) / per, most = (long long)kSms * (fit < 8 ? fit : 8) / cluster;
-    *blocks = (int)(want < most ? want : most) * cluster;
+    const int fit = resident<logprob_warp_rows_kernel<T, V, NV, SHIFT, MODE>>(kRowWarps * 32, 0);
+    const long long want = (a.rows + kRowWarps - 1) / kRowWarps, most = (long long)kSms * (fit < 8 ? fit : 8);
+    *blocks = (int)(want < most ? want : most);
+    launch(logprob_warp_rows_kernel<T, V, NV, SHIFT, MODE>, dim3(*blocks), dim3(kRowWarps * 32), 0, LaunchStream{st, true}, a);
+    return launched();
+}
+// A cluster shares a row that is longer than a stage, or that few rows leave to few blocks.  As many stages as the ring holds, up to 4.
+template <class T, bool SHIFT, int MODE> int run_block_rows(const LpArgs& a, bool dz_vec, int* blocks, cudaStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    auto kernel = logprob_block_rows_kernel<T, SHIFT, MODE>;
+    const int vecs = (a.c + (SHIFT ? V - 1 : 0) + V - 1) / V;
+    int cluster = 1;
+    auto share = [&] { return (vecs + cluster - 1) / cluster; };
+    while (share() * 16 > kStageMost) cluster *= 2;
+    while (cluster < 16 && a.rows * cluster * 2 <= kSms && share() > kBlockThreads) cluster *= 2;
+    const int stage = share() * 16, held = kRingBytes / stage;
+    const long long want = a.rows * cluster;
+    // two or three blocks an SM where their rings fit
+    const int per_sm = stage <= 16 * 1024 ? 3 : 1;
+    int stages = held / per_sm < 4 ? held / per_sm : 4;
+    const long long each = (a.rows + kSms * per_sm / cluster - 1) / (kSms * per_sm / cluster);     // rows of a block: no more stages than that
+    if (stages > each) stages = (int)each;
+    if (stages < 1) stages = 1;
+    const size_t smem = (size_t)stages * stage;
+    const long long most = (long long)(kSms * per_sm / cluster) * cluster;
+    *blocks = (int)(want < most ? want : most);
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(*blocks); cfg.blockDim = dim3(threads); cfg.stream = st;
+    cfg.gridDim = dim3(*blocks); cfg.blockDim = dim3(kBlockThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
-    if (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return FTP_ERR_CUDA;
-    if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, part) != cudaSuccess) return FTP_ERR_CUDA;
+    if (!allow_smem(kernel, smem) ||
+        (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) return FTP_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, share() * V, stages, dz_vec) != cudaSuccess) return FTP_ERR_CUDA;
     return launched();
 }
 
-// Warps hold rows of up to 1024 classes (2048 of 16 bits); blocks hold parts of up to 16384 classes (32768 of 16 bits), and a cluster shares a
-// row that is longer, or that few rows leave to few blocks.
-template <class T, int V, bool SHIFT, int MODE> int pick_rows(const LpArgs& a, int* blocks, cudaStream_t st)
-{
-    const int vecs = (a.c + (SHIFT ? V - 1 : 0) + V - 1) / V;
-    constexpr int kSmall = 8 / V ? 8 / V : 1, kMid = V == 1 ? 32 : 8, kPart = V == 1 ? 16 : 4, kWide = V == 1 ? 64 : 16;
-    if (vecs <= 32 * kSmall) return run_rows<T, V, kSmall, 32, SHIFT, MODE>(a, 1, vecs * V, blocks, st);
-    if (vecs <= 32 * kMid) return run_rows<T, V, kMid, 32, SHIFT, MODE>(a, 1, vecs * V, blocks, st);
-    int cluster = 1;
-    auto share = [&] { return (vecs + cluster - 1) / cluster; };
-    while (share() > kBlockThreads * kWide) cluster *= 2;
-    while (cluster < 16 && a.rows * cluster * 2 <= 2 * kSms && share() > kBlockThreads * kPart) cluster *= 2;
-    if (share() <= kBlockThreads * kPart) return run_rows<T, V, kPart, kBlockThreads, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
-    return run_rows<T, V, kWide, kBlockThreads, SHIFT, MODE>(a, cluster, share() * V, blocks, st);
-}
-
+// Warps hold rows of up to 1024 classes (2048 of 16 bits), blocks longer ones.
 template <class T, int MODE> int rows(const LpArgs& a, int* blocks, cudaStream_t st)
 {
     constexpr int V = 16 / sizeof(T);
@@ -767,8 +922,13 @@ template <class T, int MODE> int rows(const LpArgs& a, int* blocks, cudaStream_t
     const bool grid = aligned(a.z, 16) && (one || a.z_stride % V == 0);
     const bool same = !a.dz || (((reinterpret_cast<uintptr_t>(a.z) ^ reinterpret_cast<uintptr_t>(a.dz)) & 15) == 0 &&
                                 (one || (a.z_stride - a.dz_stride) % V == 0));
-    if (same) return grid ? pick_rows<T, V, false, MODE>(a, blocks, st) : pick_rows<T, V, true, MODE>(a, blocks, st);
-    return pick_rows<T, 1, false, MODE>(a, blocks, st);
+    const int vecs = (a.c + (grid ? 0 : V - 1) + V - 1) / V;
+    if (vecs > 32 * 8) return grid ? run_block_rows<T, false, MODE>(a, same, blocks, st) : run_block_rows<T, true, MODE>(a, same, blocks, st);
+    if (!same) return a.c <= 32 * 8 ? run_warp_rows<T, 1, 8, false, MODE>(a, blocks, st) : a.c <= 32 * 32 ? run_warp_rows<T, 1, 32, false, MODE>(a, blocks, st)
+                                                                                         : run_warp_rows<T, 1, 64, false, MODE>(a, blocks, st);
+    constexpr int kFew = 8 / V;
+    if (grid) return vecs <= 32 * kFew ? run_warp_rows<T, V, kFew, false, MODE>(a, blocks, st) : run_warp_rows<T, V, 8, false, MODE>(a, blocks, st);
+    return vecs <= 32 * kFew ? run_warp_rows<T, V, kFew, true, MODE>(a, blocks, st) : run_warp_rows<T, V, 8, true, MODE>(a, blocks, st);
 }
 
 // Warps that share a tile's classes, and classes of each: the fewest warps of up to 32 classes; 16 warps and any number of classes beyond.
