@@ -78,7 +78,7 @@ template <class T, int V> __device__ __forceinline__ void keep_packed(Pack<T, V>
 // Values [e, e + V) of an array of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as `fill`
 // and is not written.  Loads come in two steps: load_whole of all a thread's words, each one predicated instruction, then load_rest
 // where a word lies across an end.  (One function with both would put a branch between any two loads, and the next would not be
-// issued before the last has arrived.)
+// issued before the last has arrived.)  Places are ints, relative to the row or segment: wide ones cost more than the arithmetic.
 template <class T, int V> __device__ __forceinline__ Pack<T, V> filled(T fill)
 {
     Pack<T, V> r;
@@ -86,11 +86,11 @@ template <class T, int V> __device__ __forceinline__ Pack<T, V> filled(T fill)
     for (int j = 0; j < V; ++j) r.v[j] = fill;
     return r;
 }
-template <class T, int V> __device__ __forceinline__ void load_whole(Pack<T, V>& r, const T* base, long long e, long long lo, long long hi)
+template <class T, int V> __device__ __forceinline__ void load_whole(Pack<T, V>& r, const T* base, int e, int lo, int hi)
 {
     if (e >= lo && e + V <= hi) r = load_pack<T, V>(base + e);
 }
-template <class T, int V> __device__ __forceinline__ void load_rest(Pack<T, V>& r, const T* base, long long e, long long lo, long long hi)
+template <class T, int V> __device__ __forceinline__ void load_rest(Pack<T, V>& r, const T* base, int e, int lo, int hi)
 {
     if (V > 1 && e < hi && e + V > lo && (e < lo || e + V > hi)) {
 #pragma unroll
@@ -98,7 +98,7 @@ template <class T, int V> __device__ __forceinline__ void load_rest(Pack<T, V>& 
             if (e + j >= lo && e + j < hi) r.v[j] = base[e + j];
     }
 }
-template <class T, int V> __device__ __forceinline__ void store_part(T* base, long long e, long long lo, long long hi, const Pack<T, V>& a)
+template <class T, int V> __device__ __forceinline__ void store_part(T* base, int e, int lo, int hi, const Pack<T, V>& a)
 {
     if (e >= lo && e + V <= hi) { store_pack<T, V>(base + e, a); return; }
 #pragma unroll
@@ -108,14 +108,6 @@ template <class T, int V> __device__ __forceinline__ void store_part(T* base, lo
 
 // V values as fp32, in pairs where V is even: the packed fp32 instructions of sm_100 do two values in one issue slot, and all of
 // the kernels here are closer to the issue rate than to anything else but memory.
-__device__ __forceinline__ unsigned long long pair(float a, float b)
-{
-    unsigned long long r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void split(unsigned long long p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
-
 template <int V> struct Vals { float v[V]; };
 
 template <int V> __device__ __forceinline__ Vals<V> all(float s)
@@ -131,9 +123,8 @@ template <int V> __device__ __forceinline__ Vals<V> fma(const Vals<V>& a, const 
     if constexpr (V % 2 == 0) {
 #pragma unroll
         for (int j = 0; j < V; j += 2) {
-            unsigned long long d;
-            asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(pair(a.v[j], a.v[j + 1])), "l"(pair(b.v[j], b.v[j + 1])), "l"(pair(c.v[j], c.v[j + 1])));
-            split(d, r.v[j], r.v[j + 1]);
+            const float2 d = __ffma2_rn(make_float2(a.v[j], a.v[j + 1]), make_float2(b.v[j], b.v[j + 1]), make_float2(c.v[j], c.v[j + 1]));
+            r.v[j] = d.x; r.v[j + 1] = d.y;
         }
     } else {
 #pragma unroll
@@ -147,9 +138,8 @@ template <int V> __device__ __forceinline__ Vals<V> add(const Vals<V>& a, const 
     if constexpr (V % 2 == 0) {
 #pragma unroll
         for (int j = 0; j < V; j += 2) {
-            unsigned long long d;
-            asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair(a.v[j], a.v[j + 1])), "l"(pair(b.v[j], b.v[j + 1])));
-            split(d, r.v[j], r.v[j + 1]);
+            const float2 d = __fadd2_rn(make_float2(a.v[j], a.v[j + 1]), make_float2(b.v[j], b.v[j + 1]));
+            r.v[j] = d.x; r.v[j + 1] = d.y;
         }
     } else {
 #pragma unroll
@@ -163,9 +153,8 @@ template <int V> __device__ __forceinline__ Vals<V> mul(const Vals<V>& a, const 
     if constexpr (V % 2 == 0) {
 #pragma unroll
         for (int j = 0; j < V; j += 2) {
-            unsigned long long d;
-            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pair(a.v[j], a.v[j + 1])), "l"(pair(b.v[j], b.v[j + 1])));
-            split(d, r.v[j], r.v[j + 1]);
+            const float2 d = __fmul2_rn(make_float2(a.v[j], a.v[j + 1]), make_float2(b.v[j], b.v[j + 1]));
+            r.v[j] = d.x; r.v[j + 1] = d.y;
         }
     } else {
 #pragma unroll

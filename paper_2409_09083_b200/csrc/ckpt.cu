@@ -22,12 +22,6 @@ struct CkptArgs {
 constexpr int kThreads = 256;
 constexpr int kPer = 4;             // vectors of a lane in a segment
 
-template <class T, int V> __device__ __forceinline__ T* run_at(const CkptArgs& a, long long run)
-{
-    const long long n = run / a.per_sample;
-    return static_cast<T*>(a.x) + n * a.sample_stride + (run - n * a.per_sample) * a.run_stride;
-}
-
 template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads) ckpt_kernel(CkptArgs a, long long segments)
 {
     previous_launches();
@@ -35,63 +29,66 @@ template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads)
     const int lane = threadIdx.x & 31;
     const long long warps = (long long)gridDim.x * (kThreads / 32);
     for (long long task = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); task < a.runs * segments; task += warps) {
-        const long long run = segments == 1 ? task : task / segments;
-        const long long first = (task - run * segments) * kSegment + lane * V;
-        T* x = run_at<T, V>(a, run);
-        unsigned char* q = a.ck.q + run * a.ck.pitch;
-        unsigned char* steps = a.ck.steps + run * a.ck.blocks;
+        const long long run = segments == 1 ? task : task / segments, start = (task - run * segments) * kSegment;
+        const long long n = a.per_sample == 1 ? run : run / a.per_sample;
+        // from here on places are relative to the segment
+        T* x = static_cast<T*>(a.x) + n * a.sample_stride + (run - n * a.per_sample) * a.run_stride + start;
+        unsigned char* q = a.ck.q + run * a.ck.pitch + start;
+        unsigned char* steps = a.ck.steps + run * a.ck.blocks + (start >> 5);
+        const int len = (int)(a.len - start < kSegment ? a.len - start : kSegment), padded = (int)(a.ck.pitch - start < kSegment ? a.ck.pitch - start : kSegment);
         if constexpr (SAVE) {
             Pack<T, V> raw[kPer];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const long long e = first + i * 32 * V;
                 raw[i] = zero_pack<T, V>();
-                load_whole<T, V>(raw[i], x, e, 0, a.len);
+                load_whole<T, V>(raw[i], x, (i * 32 + lane) * V, 0, len);
             }
-            if (a.len % V) {
+            if (V > 1 && len % V) {
 #pragma unroll
-                for (int i = 0; i < kPer; ++i) load_rest<T, V>(raw[i], x, first + i * 32 * V, 0, a.len);
+                for (int i = 0; i < kPer; ++i) load_rest<T, V>(raw[i], x, (i * 32 + lane) * V, 0, len);
             }
             // every block as if it held finite values only, then the others again
+            float big[kPer];
             bool any = false;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const long long e = first + i * 32 * V;
-                const Vals<V> v = values(raw[i]);
-                const float big = largest(v);
-                any |= special<T>(big);
-                const unsigned ex = step_exponent(big);
-                if (e < a.ck.pitch) {
-                    store_pack<unsigned char, V>(q + e, to_steps(v, ex));
-                    if (e % kBlock == 0) steps[e / kBlock] = (unsigned char)ex;
+                big[i] = largest(values(raw[i]));
+                any |= special<T>(big[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int e = (i * 32 + lane) * V;
+                const unsigned ex = step_exponent(big[i]);
+                if (e < padded) {
+                    store_pack<unsigned char, V>(q + e, to_steps(values(raw[i]), ex));
+                    if (lane % (kBlock / V) == 0) steps[(unsigned)e >> 5] = (unsigned char)ex;
                 }
             }
             if (!__any_sync(0xffffffffu, any)) continue;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const long long e = first + i * 32 * V;
-                const Vals<V> v = values(raw[i]);
-                if (!special<T>(largest(v))) continue;
+                const int e = (i * 32 + lane) * V;
+                if (!special<T>(big[i])) continue;
                 unsigned ex;
-                const Pack<unsigned char, V> b = to_steps_special<T, V>(v, ex);
-                if (e < a.ck.pitch) {
+                const Pack<unsigned char, V> b = to_steps_special<T, V>(values(raw[i]), ex);
+                if (e < padded) {
                     store_pack<unsigned char, V>(q + e, b);
-                    if (e % kBlock == 0) steps[e / kBlock] = (unsigned char)ex;
+                    if (lane % (kBlock / V) == 0) steps[(unsigned)e >> 5] = (unsigned char)ex;
                 }
             }
         } else {
             Pack<unsigned char, V> b[kPer];
-            unsigned char ex[kPer];
+            unsigned ex[kPer];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const long long e = first + i * 32 * V;
-                if (e < a.len) { b[i] = load_pack<unsigned char, V>(q + e); ex[i] = steps[e / kBlock]; }
+                const int e = (i * 32 + lane) * V;
+                ex[i] = 1;
+                if (e < len) { b[i] = load_pack<unsigned char, V>(q + e); ex[i] = steps[(unsigned)e >> 5]; }
             }
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                const long long e = first + i * 32 * V;
-                if (e >= a.len) continue;
-                store_part<T, V>(x, e, 0, a.len, rounded<T, V>(mul(steps_of(b[i]), all<V>(step_of(ex[i])))));
+                const int e = (i * 32 + lane) * V;
+                if (e < len) store_part<T, V>(x, e, 0, len, rounded<T, V>(mul(steps_of(b[i]), all<V>(step_of(ex[i])))));
             }
         }
     }

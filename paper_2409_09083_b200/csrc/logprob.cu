@@ -23,7 +23,6 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLeast = -160.f;                       // 2^-160 is 0 in fp32: where a = -inf would make 0 * inf
 constexpr int kTop = FTP_TOP_MAX;
 constexpr int kParts = 32;                             // parts of a row, whose maxima bound its best values
-constexpr int kBlockThreads = 512;
 constexpr int kListBlock = 512, kListWarp = 64;        // candidates
 constexpr int kCountHere = 4096;                       // rows whose labels every block counts by itself
 
@@ -347,10 +346,12 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
     }
 }
 
-// Longer rows: a block of 512 threads has a row, or with a cluster its part of one, in shared memory, and the next ones are on their way
-// into the other stages.  A thread copies (cp.async, 16 bytes each) what it will read itself, every 512th vector, so that no barrier
-// stands between copy and use, and the passes over the row are short loops: with the row in registers instead they had to be unrolled
-// in full and waited for instructions more than for anything else (4096 x 32000 bf16 with the eight best: 159 us).
+// Longer rows: TH threads of a block have a row, or with a cluster its part of one, in shared memory, and the next ones are on their
+// way into the other stages.  A thread copies (cp.async, 16 bytes each) what it will read itself, every TH-th vector, so that no barrier
+// stands between copy and use, and the passes over the row are short loops: with the row in registers instead they had to be
+// unrolled in full and waited for instructions more than for anything else (4096 x 32000 bf16 with the eight best: 159 us).
+// What is left to do for a row once its sums and its list of candidates are there, a thousand cycles of one warp, is one more warp's
+// (FIN), while the others are at the next row.  Blocks of a cluster, and the loss, whose delta needs the sums at once, do without.
 constexpr int kStageMost = 64 * 1024;            // bytes of a part: 32768 classes of 16 bits, 16384 of 32
 constexpr int kRingBytes = 200 * 1024;
 
@@ -374,126 +375,152 @@ __device__ __forceinline__ void wait_rows(int left)
 {
     if (left <= 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
     else if (left == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (left == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
 
-template <class T, bool SHIFT, int MODE>
-__global__ void __launch_bounds__(kBlockThreads, 1) logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_vec)
+template <class T, bool SHIFT, int MODE, int TH, bool FIN>
+__global__ void __launch_bounds__(TH + (FIN ? 32 : 0), TH == 128 ? 3 : 1)
+logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_vec)
 {
-    constexpr int V = 16 / sizeof(T), kWarps = kBlockThreads / 32, kLanes = kBlockThreads / kParts;
+    constexpr int V = 16 / sizeof(T), kWarps = TH / 32, kLanes = TH / kParts, kStep = TH * V, kAll = TH + (FIN ? 32 : 0);
     extern __shared__ __align__(16) unsigned char ring[];
     __shared__ BlockShared sh;
     previous_launches();
     const int t = threadIdx.x, lane = t & 31;
-    const int rank = (int)(blockIdx.x % cluster);
-    const long long step = gridDim.x / cluster;
+    const int rank = FIN ? 0 : (int)(blockIdx.x % cluster);
+    const long long step = FIN ? gridDim.x : gridDim.x / cluster;
     const bool want_top = MODE == kStats && a.top > 0;
     float over = 0.f, total = 0.f;
     if (MODE == kLoss) {
         const float k = labelled_rows(a);
         over = k > 0.f ? a.scale / k : 0.f;
     }
+    if (t < 2) sh.count[t] = 0;
+    __syncthreads();
+    long long row = FIN ? blockIdx.x : blockIdx.x / cluster;
+    int turn = 0;
+    auto sync_rows = [&] { if constexpr (FIN) group_barrier(1, kAll); else __syncthreads(); };
+    auto sync_list = [&] { if constexpr (FIN) group_barrier(2, kAll); else __syncthreads(); };
+    if (FIN && t >= TH) {
+        for (; row < a.rows; row += step, turn ^= 1) {
+            Label label{-1, 0.f, 0};
+            if (lane == 0) label = read_label<T>(a, row, static_cast<const T*>(a.z) + row * a.z_stride, 1);
+            sync_rows();                         // (this also says that the list of the row before has been read)
+            const RowResult r = result_of(join_lanes(sh.sums[turn], kWarps));
+            if (lane == 0) write_stats(a, row, r, label);
+            if (!want_top) continue;
+            sync_list();
+            int found = sh.count[turn];
+            if (found > kListBlock) { sync_list(); found = a.top; }
+            place(sh.list, found, a.top, lane, 32, [&](int at, unsigned long long k) {
+                if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
+                if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
+            });
+        }
+        return;
+    }
     auto shift_of = [&](const T* zr) { return SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0; };
-    // places [first, last) of the row, on the grid that starts o below it, are this block's
+    // places [first, last) of the row, on the grid that starts o below it, are this block's; a thread's vectors start at first + t V + k kStep
     auto fetch = [&](long long row, int stage) {
         if (row < a.rows) {
             const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
-            const int o = shift_of(zr), first = rank * part, last = min(o + a.c, first + part);
-            T* to = reinterpret_cast<T*>(ring + (size_t)stage * part * sizeof(T));
+            const int o = shift_of(zr), first = rank * part, last = min(o + a.c, first + part), mine = last - first - t * V;
+            T* to = reinterpret_cast<T*>(ring + (size_t)stage * part * sizeof(T)) + t * V;
             zr -= o;
-            for (int e = first + t * V; e < last; e += kBlockThreads * V) {
-                if (e >= o && e + V <= last) copy_16(to + (e - first), zr + e);
-                else {
-                    Pack<T, V> p = filled<T, V>(from_f<T>(minus_inf()));
-                    load_rest<T, V>(p, zr, e, o, last);
-                    store_pack<T, V>(to + (e - first), p);
-                }
-            }
+            const T* from = zr + first + t * V;
+            const int whole = mine < V ? 0 : (mine - V) / kStep + 1;                    // vectors that end before `last`
+            const bool head = SHIFT && o > 0 && rank == 0 && t == 0;                    // the first one starts before the row
+#pragma unroll 4
+            for (int k = head ? 1 : 0; k < whole; ++k) copy_16(to + k * kStep, from + k * kStep);
+            auto across = [&](int k) {
+                Pack<T, V> p = filled<T, V>(from_f<T>(minus_inf()));
+                load_rest<T, V>(p, zr, first + t * V + k * kStep, o, last);
+                store_pack<T, V>(to + k * kStep, p);
+            };
+            if (head) across(0);
+            if (whole * kStep < mine && !(head && whole == 0)) across(whole);
         }
         copies_of_row_end();
     };
-    long long row = blockIdx.x / cluster;
     for (int i = 0; i + 1 < stages; ++i) fetch(row + i * step, i);
-    if (t < 2) sh.count[t] = 0;
-    __syncthreads();
-    int turn = 0, stage = 0;
+    int stage = 0;
     for (; row < a.rows; row += step, turn ^= 1) {
         const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
         const int o = shift_of(zr), first = rank * part, last = min(o + a.c, first + part);
         const T* mine_at = reinterpret_cast<const T*>(ring + (size_t)stage * part * sizeof(T)) + t * V;
-        const int count = last - first;                          // places from the part's start; a thread's are t V, t V + 512 V, ..
+        const int vectors = max(0, (last - first - t * V + kStep - 1) / kStep);
         Label label{-1, 0.f, 0};
-        if (MODE == kLoss || t == 0) label = read_label<T>(a, row, zr, 1);
+        if (!FIN && (MODE == kLoss || t == 0)) label = read_label<T>(a, row, zr, 1);
         fetch(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
         wait_rows(stages - 1);
         stage = stage + 1 == stages ? 0 : stage + 1;
         Largest<T, V> most;
 #pragma unroll 4
-        for (int e = t * V, k = 0; e < count; e += kBlockThreads * V, ++k) most.take(load_pack<T, V>(mine_at + k * kBlockThreads * V));
+        for (int k = 0; k < vectors; ++k) most.take(load_pack<T, V>(mine_at + k * kStep));
         const float mine = most.value();
         // largest of a part of the row, and of the warp, which the exponents are taken from
-        float part_max = lanes_max(mine, kLanes);
+        const float part_max = lanes_max(mine, kLanes);
         if (want_top && lane % kLanes == 0) sh.parts[t / kLanes] = part_max;
         const float m = lanes_max(part_max), shift = m == minus_inf() ? 0.f : m;
         Vals<V> s = all<V>(0.f), x2 = all<V>(0.f);
 #pragma unroll 4
-        for (int e = t * V, k = 0; e < count; e += kBlockThreads * V, ++k)
-            take_sums<MODE, V>(values(load_pack<T, V>(mine_at + k * kBlockThreads * V)), shift, s, x2);
+        for (int k = 0; k < vectors; ++k) take_sums<MODE, V>(values(load_pack<T, V>(mine_at + k * kStep)), shift, s, x2);
         Sums sums{shift, lanes_sum(sum_of(s)), 0.f};
         if (MODE == kStats) sums.t = lanes_sum(sum_of(x2));
         if (lane == 0) sh.sums[turn][t >> 5] = sums;
-        __syncthreads();
-        if (t < 32 || MODE == kLoss || cluster > 1) sums = join_lanes(sh.sums[turn], kWarps);
+        sync_rows();
+        if (!FIN && (t < 32 || MODE == kLoss || cluster > 1)) sums = join_lanes(sh.sums[turn], kWarps);
         if (t == 0) sh.count[turn ^ 1] = 0;
         // the best classes of this part
         int found = 0;
         if (want_top) {
             const float bound = bound_of(sh.parts[lane], a.top);
             if (mine >= bound) {
-                for (int e = t * V, k = 0; e < count; e += kBlockThreads * V, ++k) {
-                    const Pack<T, V> p = load_pack<T, V>(mine_at + k * kBlockThreads * V);
+                for (int k = 0; k < vectors; ++k) {
+                    const Pack<T, V> p = load_pack<T, V>(mine_at + k * kStep);
                     Largest<T, V> here;
                     here.take(p);
                     if (here.value() < bound) continue;
+                    const int e = first + t * V + k * kStep;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float v = fmaxf(to_f(p.v[j]), minus_inf());
-                        const int place = first + e + j;
-                        if (v >= bound && place >= o && place < last) {
+                        if (v >= bound && e + j >= o && e + j < last) {
                             const int at = atomicAdd(&sh.count[turn], 1);
-                            if (at < kListBlock) sh.list[at] = key_of(v, place - o);
+                            if (at < kListBlock) sh.list[at] = key_of(v, e + j - o);
                         }
                     }
                 }
             }
-            __syncthreads();
+            sync_list();
             found = sh.count[turn];
             if (found > kListBlock) {                             // too many equal ones: one place after the other
                 unsigned long long before = ~0ull;
                 const int places = min(a.top, found);
                 for (int k = 0; k < places; ++k) {
                     unsigned long long best = 0;
-                    for (int e = t; e < count; e += kBlockThreads) {
-                        const unsigned long long key = first + e >= o ? key_of(to_f(zr[first + e - o]), first + e - o) : 0ull;
+                    for (int e = max(first, o) + t; e < last; e += TH) {
+                        const unsigned long long key = key_of(to_f(zr[e - o]), e - o);
                         if (key < before && key > best) best = key;
                     }
                     best = lanes_best(best, 32);
-                    __syncthreads();
+                    group_barrier(3, TH);
                     if (lane == 0) sh.round[t >> 5] = best;
-                    __syncthreads();
+                    group_barrier(3, TH);
                     before = lanes_best(sh.round[lane & (kWarps - 1)], 32);
                     if (t == 0) sh.list[k] = before;
                 }
                 found = places;
-                __syncthreads();
+                sync_list();
             }
         }
-        if (cluster > 1) {
+        if (!FIN && cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (want_top) {
                 if (t < kTop) sh.best[t] = 0;
                 __syncthreads();
-                place(sh.list, found, a.top, t, kBlockThreads, [&](int at, unsigned long long k) { sh.best[at] = k; });
+                place(sh.list, found, a.top, t, TH, [&](int at, unsigned long long k) { sh.best[at] = k; });
             }
             if (t == 0) sh.whole = sums;
             cl.sync();
@@ -501,29 +528,30 @@ __global__ void __launch_bounds__(kBlockThreads, 1) logprob_block_rows_kernel(Lp
             for (int r = 1; r < cluster; ++r) sums = join(sums, *cl.map_shared_rank(&sh.whole, r));
             if (want_top && rank == 0) {
                 found = cluster * a.top;
-                for (int i = t; i < found; i += kBlockThreads) sh.list[i] = cl.map_shared_rank(sh.best, i / a.top)[i % a.top];
+                for (int i = t; i < found; i += TH) sh.list[i] = cl.map_shared_rank(sh.best, i / a.top)[i % a.top];
                 __syncthreads();
             }
         }
-        const RowResult r = result_of(sums);
-        if (MODE == kStats && rank == 0) {
+        if (!FIN && MODE == kStats && rank == 0) {                // (cluster > 1: a row alone has the warp above)
+            const RowResult r = result_of(sums);
             if (t == 0) write_stats(a, row, r, label);
-            auto best_of_row = [&](int at, unsigned long long k) {
-                if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
-                if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
-            };
-            if (want_top && cluster > 1) place(sh.list, found, a.top, t, kBlockThreads, best_of_row);
-            else if (want_top && t < 32) place(sh.list, found, a.top, t, 32, best_of_row);        // (this warp alone knows the row's sums)
+            if (want_top)
+                place(sh.list, found, a.top, t, TH, [&](int at, unsigned long long k) {
+                    if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
+                    if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
+                });
         }
         if (MODE == kLoss) {
+            const RowResult r = result_of(sums);
             if (t == 0 && rank == 0 && label.has) total += logp_of_label(r, label);
             if (a.dz) {
                 T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
                 const float f = label.has > 0 ? (r.empty ? 0.f : over) : label.has == 0 ? 0.f : nan_f(), g = f == 0.f ? 0.f : f / sums.s;
                 const int at = label.has > 0 ? (int)label.cls + o : -1;
 #pragma unroll 2
-                for (int k = 0, e = first + t * V; e < last; e += kBlockThreads * V, ++k) {
-                    const Pack<T, V> d = rounded<T, V>(loss_grads(values(load_pack<T, V>(mine_at + k * kBlockThreads * V)), sums.m, g, f, e, at));
+                for (int k = 0; k < vectors; ++k) {
+                    const int e = first + t * V + k * kStep;
+                    const Pack<T, V> d = rounded<T, V>(loss_grads(values(load_pack<T, V>(mine_at + k * kStep)), sums.m, g, f, e, at));
                     if (dz_vec) store_part<T, V>(dr, e, o, last, d);
                     else {
 #pragma unroll
@@ -533,7 +561,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) logprob_block_rows_kernel(Lp
                 }
             }
         }
-        if (cluster > 1) cg::this_cluster().sync();               // the others read this block's part
+        if (!FIN && cluster > 1) cg::this_cluster().sync();       // the others read this block's part
     }
     wait_rows(0);
     if (MODE == kLoss && a.sums && t == 0) a.sums[blockIdx.x] = total;
@@ -879,39 +907,45 @@ template <class T, int V, int NV, bool SHIFT, int MODE> int run_warp_rows(const 
     launch(logprob_warp_rows_kernel<T, V, NV, SHIFT, MODE>, dim3(*blocks), dim3(kRowWarps * 32), 0, LaunchStream{st, true}, a);
     return launched();
 }
-// A cluster shares a row that is longer than a stage, or that few rows leave to few blocks.  As many stages as the ring holds, up to 4.
-template <class T, bool SHIFT, int MODE> int run_block_rows(const LpArgs& a, bool dz_vec, int* blocks, cudaStream_t st)
+template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(const LpArgs& a, int cluster, int share, bool dz_vec, int* blocks, cudaStream_t st)
 {
-    constexpr int V = 16 / sizeof(T);
-    auto kernel = logprob_block_rows_kernel<T, SHIFT, MODE>;
-    const int vecs = (a.c + (SHIFT ? V - 1 : 0) + V - 1) / V;
-    int cluster = 1;
-    auto share = [&] { return (vecs + cluster - 1) / cluster; };
-    while (share() * 16 > kStageMost) cluster *= 2;
-    while (cluster < 16 && a.rows * cluster * 2 <= kSms && share() > kBlockThreads) cluster *= 2;
-    const int stage = share() * 16, held = kRingBytes / stage;
-    const long long want = a.rows * cluster;
-    // two or three blocks an SM where their rings fit
-    const int per_sm = stage <= 16 * 1024 ? 3 : 1;
-    int stages = held / per_sm < 4 ? held / per_sm : 4;
-    const long long each = (a.rows + kSms * per_sm / cluster - 1) / (kSms * per_sm / cluster);     // rows of a block: no more stages than that
+    auto kernel = logprob_block_rows_kernel<T, SHIFT, MODE, TH, FIN>;
+    const int threads = TH + (FIN ? 32 : 0), stage = share * 16;
+    // rings of two stages at least, and of up to four where all the blocks that the registers allow still fit
+    int fit = resident<logprob_block_rows_kernel<T, SHIFT, MODE, TH, FIN>>(threads, 0);
+    while (fit > 1 && 2 * fit * stage > kRingBytes) --fit;
+    int stages = kRingBytes / (fit * stage);
+    if (stages > 4) stages = 4;
+    const long long slots = (long long)kSms * fit / cluster, each = (a.rows + slots - 1) / slots;      // rows of a block: no more stages than that
     if (stages > each) stages = (int)each;
-    if (stages < 1) stages = 1;
     const size_t smem = (size_t)stages * stage;
-    const long long most = (long long)(kSms * per_sm / cluster) * cluster;
-    *blocks = (int)(want < most ? want : most);
+    *blocks = (int)(a.rows < slots ? a.rows : slots) * cluster;
     cudaLaunchAttribute at[2] = {};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(*blocks); cfg.blockDim = dim3(kBlockThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.gridDim = dim3(*blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (!allow_smem(kernel, smem) ||
         (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) return FTP_ERR_CUDA;
-    if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, share() * V, stages, dz_vec) != cudaSuccess) return FTP_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, share * (int)(16 / sizeof(T)), stages, dz_vec) != cudaSuccess) return FTP_ERR_CUDA;
     return launched();
+}
+// A cluster shares a row that is longer than a stage, or that few rows leave to few blocks; rows of up to 16 KB take 128 threads.
+template <class T, bool SHIFT, int MODE> int pick_block_rows(const LpArgs& a, bool dz_vec, int* blocks, cudaStream_t st)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int vecs = (a.c + (SHIFT ? V - 1 : 0) + V - 1) / V;
+    int cluster = 1;
+    auto share = [&] { return (vecs + cluster - 1) / cluster; };
+    while (share() * 16 > kStageMost) cluster *= 2;
+    while (cluster < 16 && a.rows * cluster * 2 <= kSms && share() > 512) cluster *= 2;
+    constexpr bool kFin = MODE == kStats;
+    if (cluster > 1) return run_block_rows<T, SHIFT, MODE, 512, false>(a, cluster, share(), dz_vec, blocks, st);
+    if (share() <= 1024) return run_block_rows<T, SHIFT, MODE, 128, kFin>(a, 1, share(), dz_vec, blocks, st);
+    return run_block_rows<T, SHIFT, MODE, 512, kFin>(a, 1, share(), dz_vec, blocks, st);
 }
 
 // Warps hold rows of up to 1024 classes (2048 of 16 bits), blocks longer ones.
@@ -923,7 +957,7 @@ template <class T, int MODE> int rows(const LpArgs& a, int* blocks, cudaStream_t
     const bool same = !a.dz || (((reinterpret_cast<uintptr_t>(a.z) ^ reinterpret_cast<uintptr_t>(a.dz)) & 15) == 0 &&
                                 (one || (a.z_stride - a.dz_stride) % V == 0));
     const int vecs = (a.c + (grid ? 0 : V - 1) + V - 1) / V;
-    if (vecs > 32 * 8) return grid ? run_block_rows<T, false, MODE>(a, same, blocks, st) : run_block_rows<T, true, MODE>(a, same, blocks, st);
+    if (vecs > 32 * 8) return grid ? pick_block_rows<T, false, MODE>(a, same, blocks, st) : pick_block_rows<T, true, MODE>(a, same, blocks, st);
     if (!same) return a.c <= 32 * 8 ? run_warp_rows<T, 1, 8, false, MODE>(a, blocks, st) : a.c <= 32 * 32 ? run_warp_rows<T, 1, 32, false, MODE>(a, blocks, st)
                                                                                          : run_warp_rows<T, 1, 64, false, MODE>(a, blocks, st);
     constexpr int kFew = 8 / V;

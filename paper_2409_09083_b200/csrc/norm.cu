@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
                 const unsigned ex = step_exponent(big);
                 if (live && e < a.ck.pitch) {
                     store_pack<unsigned char, V>(qr + skip, to_steps(v, ex));
-                    if (e % kBlock == 0) er[skip / kBlock] = (unsigned char)ex;
+                    if (t % (kBlock / V) == 0) er[(unsigned)skip / kBlock] = (unsigned char)ex;
                 }
             }
             if (e < hi) {
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
                 const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
                 if (live && e < a.ck.pitch) {
                     store_pack<unsigned char, V>(qr + skip, st);
-                    if (e % kBlock == 0) er[skip / kBlock] = (unsigned char)ex;
+                    if (t % (kBlock / V) == 0) er[(unsigned)skip / kBlock] = (unsigned char)ex;
                 }
             }
         }
@@ -272,7 +272,7 @@ __device__ __forceinline__ void load_row(const RowAt<T>& at, bool live, int c, i
             else load_whole<T, V>(in.dy[i], at.dy - t * V, e, 0, c);
             if constexpr (CK) {
                 in.x[i].q = load_pack<unsigned char, V>(at.q + skip);
-                in.x[i].e = at.e[skip / kBlock];
+                in.x[i].e = at.e[(unsigned)skip / kBlock];
             } else {
                 if (kWhole) in.x[i].a = load_pack<T, V>(at.x + skip);
                 else load_whole<T, V>(in.x[i].a, at.x - t * V, e, 0, c);
