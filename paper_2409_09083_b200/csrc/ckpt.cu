@@ -22,14 +22,13 @@ struct CkptArgs {
 constexpr int kThreads = 256;
 constexpr int kPer = 4;             // vectors of a lane in a segment
 
-template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads) ckpt_kernel(CkptArgs a, long long segments)
+template <class T, int V, bool SAVE> __global__ void __launch_bounds__(kThreads) ckpt_kernel(CkptArgs a, int segments)
 {
     previous_launches();
     constexpr int kSegment = 32 * V * kPer;
     const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * (kThreads / 32);
-    for (long long task = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); task < a.runs * segments; task += warps) {
-        const long long run = segments == 1 ? task : task / segments, start = (task - run * segments) * kSegment;
+    for (Walk w(blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), gridDim.x * (kThreads / 32), segments); w.hi < a.runs; w.advance()) {
+        const long long run = w.hi, start = (long long)w.lo * kSegment;
         const long long n = a.per_sample == 1 ? run : run / a.per_sample;
         // from here on places are relative to the segment
         T* x = static_cast<T*>(a.x) + n * a.sample_stride + (run - n * a.per_sample) * a.run_stride + start;
@@ -98,7 +97,7 @@ template <class T, int V, bool SAVE> int run(const CkptArgs& a, LaunchStream ls)
 {
     const long long segment = 32 * V * kPer, segments = (a.ck.pitch + segment - 1) / segment, tasks = a.runs * segments;
     const long long want = (tasks + kThreads / 32 - 1) / (kThreads / 32), most = 8LL * kSms;
-    launch(ckpt_kernel<T, V, SAVE>, dim3((unsigned)(want < most ? want : most)), dim3(kThreads), 0, ls, a, segments);
+    launch(ckpt_kernel<T, V, SAVE>, dim3((unsigned)(want < most ? want : most)), dim3(kThreads), 0, ls, a, (int)segments);
     return launched();
 }
 template <class T, bool SAVE> int pick(const CkptArgs& a, LaunchStream ls)
@@ -118,9 +117,12 @@ template <bool SAVE> int ckpt(const ftp_dims* d, const void* x, long long x_stri
     CkptArgs a{};
     a.x = const_cast<void*>(x); a.ck = ckpt_view(d, ck);
     a.len = run_length(d); a.runs = run_count(d); a.run_stride = a.len; a.sample_stride = x_stride; a.per_sample = d->p == 1 ? 1 : d->c;
-    if (a.len % kBlock == 0 && (x_stride == d->c * d->p || d->n == 1) && a.runs * a.ck.blocks < (1LL << 31)) {
-        a.len *= a.runs; a.ck.pitch *= a.runs; a.ck.blocks *= (int)a.runs;
-        a.runs = a.per_sample = 1;
+    if (x_stride == d->c * d->p || d->n == 1) {
+        a.per_sample = 1; a.sample_stride = a.len;            // runs lie one behind the other
+        if (a.len % kBlock == 0 && a.runs * a.ck.blocks < (1LL << 31)) {
+            a.len *= a.runs; a.ck.pitch *= a.runs; a.ck.blocks *= (int)a.runs;
+            a.runs = 1;
+        }
     }
     const LaunchStream ls{static_cast<cudaStream_t>(stream), true};
     if (d->type == FTP_TYPE_F32) return pick<float, SAVE>(a, ls);

@@ -143,7 +143,7 @@ template <class T, int V> struct Largest {
     __device__ __forceinline__ void take(const Pack<T, V>& p)
     {
 #pragma unroll
-        for (int j = 0; j < V; ++j) v = fmaxf(v, to_f(p.v[j]));
+        for (int j = 0; j < V; ++j) v = fmaxf(v, to_f(p.get(j)));
     }
     __device__ __forceinline__ float value() const { return v; }
 };
@@ -154,8 +154,7 @@ template <class T, class T2> struct LargestPairs {
     __device__ __forceinline__ LargestPairs() { v.x = v.y = from_f<T>(minus_inf()); }
     __device__ __forceinline__ void take(const Pack<T, 8>& p)
     {
-        T2 w[4];
-        __builtin_memcpy(w, &p, 16);
+        const T2* w = reinterpret_cast<const T2*>(p.w);
         v = max_two(v, max_two(max_two(w[0], w[1]), max_two(w[2], w[3])));
     }
     __device__ __forceinline__ float value() const { return fmaxf(to_f(v.x), to_f(v.y)); }
@@ -206,17 +205,23 @@ __device__ __forceinline__ Sums join_lanes(const Sums* of, int n)
     return s;
 }
 
-// Adds a vector's exponents to the sums of a thread.
-template <int MODE, int V> __device__ __forceinline__ void take_sums(const Vals<V>& z, float shift, Vals<V>& s, Vals<V>& t)
+// Adds a vector's exponents to the sums of a thread, which are A side by side.
+template <int MODE, int V, int A> __device__ __forceinline__ void take_sums(const Vals<V>& z, float shift, Vals<A>& s, Vals<A>& t)
 {
-    Vals<V> x = mul(add(z, all<V>(-shift)), all<V>(kLog2e)), e;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        if (MODE == kStats) x.v[j] = max_nan(x.v[j], kLeast);
-        e.v[j] = ex2(x.v[j]);
+    for (int i = 0; i < V; i += A) {
+        Vals<A> x, e;
+#pragma unroll
+        for (int j = 0; j < A; ++j) x.v[j] = z.v[i + j];
+        x = mul(add(x, all<A>(-shift)), all<A>(kLog2e));
+#pragma unroll
+        for (int j = 0; j < A; ++j) {
+            if (MODE == kStats) x.v[j] = max_nan(x.v[j], kLeast);
+            e.v[j] = ex2(x.v[j]);
+        }
+        s = add(s, e);
+        if (MODE == kStats) t = fma(e, x, t);
     }
-    s = add(s, e);
-    if (MODE == kStats) t = fma(e, x, t);
 }
 
 // dlogits of a vector of places e ..: g 2^((z - m) log2 e), less f at the label's place `at`; 0 if f is.
@@ -233,6 +238,25 @@ template <int V> __device__ __forceinline__ Vals<V> loss_grads(const Vals<V>& z,
             if (e + j == at) x.v[j] -= f;
     }
     return x;
+}
+
+// How many keys a warp's list holds.  Where equal values overflowed it, the best classes take their places one after the other.
+template <class T> __device__ __forceinline__ int best_of_list(const LpArgs& a, const T* zr, int found, unsigned long long* list, int lane)
+{
+    if (found <= kListWarp) return found;
+    unsigned long long before = ~0ull;
+    __syncwarp();
+    for (int k = 0; k < a.top; ++k) {
+        unsigned long long best = 0;
+        for (int e = lane; e < a.c; e += 32) {
+            const unsigned long long key = key_of(to_f(zr[e]), e);
+            if (key < before && key > best) best = key;
+        }
+        before = lanes_best(best, 32);
+        if (lane == 0) list[k] = before;
+    }
+    __syncwarp();
+    return a.top;
 }
 
 // Rows that a warp holds in its registers, as NV vectors of V logits a lane.  SHIFT as in norm.cu: vectors lie on the 16-byte grid below
@@ -276,7 +300,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
         const float mine = most.value(), m = lanes_max(mine), shift = m == minus_inf() ? 0.f : m;
         Vals<V> s = all<V>(0.f), x2 = all<V>(0.f);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) take_sums<MODE, V>(values(raw[i]), shift, s, x2);
+        for (int i = 0; i < NV; ++i) take_sums<MODE>(values(raw[i]), shift, s, x2);
         Sums sums{shift, lanes_sum(sum_of(s)), 0.f};
         if (MODE == kStats) sums.t = lanes_sum(sum_of(x2));
         const RowResult r = result_of(sums);
@@ -291,7 +315,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
                     const int e = (i * 32 + lane) * V;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float v = fmaxf(to_f(raw[i].v[j]), minus_inf());
+                        const float v = fmaxf(to_f(raw[i].get(j)), minus_inf());
                         if (v >= bound && e + j >= o && e + j < last) {
                             const int at = atomicAdd(count, 1);
                             if (at < kListWarp) list[at] = key_of(v, e + j - o);
@@ -300,21 +324,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
                 }
             }
             __syncwarp();
-            int found = *count;
-            if (found > kListWarp) {                              // too many equal ones: one place after the other
-                unsigned long long before = ~0ull;
-                for (int k = 0; k < a.top; ++k) {
-                    unsigned long long best = 0;
-                    for (int e = lane; e < a.c; e += 32) {
-                        const unsigned long long key = key_of(to_f(zr[e]), e);
-                        if (key < before && key > best) best = key;
-                    }
-                    before = lanes_best(best, 32);
-                    if (lane == 0) list[k] = before;
-                }
-                found = a.top;
-                __syncwarp();
-            }
+            const int found = best_of_list<T>(a, zr, *count, list, lane);
             place(list, found, a.top, lane, 32, [&](int at, unsigned long long k) {
                 if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
                 if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
@@ -343,6 +353,115 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
             for (int i = 0; i < kRowWarps; ++i) s += totals[i];
             a.sums[blockIdx.x] = s;
         }
+    }
+}
+
+// Many long rows: a warp streams a row, four vectors a lane at a time with the next four on their way, and keeps a running maximum that
+// the sums are brought to when it grows.  Without barriers, and with what a row costs once (400 instructions) spread over all of its values
+// in a lane: 4096 x 32000 bf16 with the eight best take 122 us with a block a row.  The row is cut into up to 32 units of batches, and the
+// largest value of each lane in each unit stays in shared memory: where one reaches the bound, the whole warp looks the lane's values over.
+constexpr int kStreamWarps = 4, kBatch = 4, kUnits = 32;
+
+template <class T, bool SHIFT> __global__ void __launch_bounds__(kStreamWarps * 32, 7) logprob_stream_rows_kernel(LpArgs a)
+{
+    constexpr int V = 16 / sizeof(T), kWide = 32 * V * kBatch;              // places of a batch
+    __shared__ unsigned long long lists[kStreamWarps][kListWarp];
+    __shared__ int counts[kStreamWarps];
+    __shared__ float largest_of[kStreamWarps][kUnits][32];
+    previous_launches();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned long long* list = lists[warp];
+    int* count = counts + warp;
+    for (long long row = (long long)blockIdx.x * kStreamWarps + warp; row < a.rows; row += (long long)gridDim.x * kStreamWarps) {
+        const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
+        const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0, last = o + a.c;
+        const int batches = (last + kWide - 1) / kWide, unit = (batches + kUnits - 1) / kUnits, units = (batches + unit - 1) / unit;
+        const T* grid = zr - o;
+        Label label{-1, 0.f, 0};
+        if (lane == 0) label = read_label<T>(a, row, zr, 1);
+        Pack<T, V> next[kBatch];
+        auto fetch = [&](int b) {
+            const int e = b * kWide + lane * V;
+            if ((!SHIFT || b > 0) && (b + 1) * kWide <= last) {
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) next[i] = load_pack<T, V>(grid + e + i * 32 * V);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    next[i] = filled<T, V>(from_f<T>(minus_inf()));
+                    load_whole<T, V>(next[i], grid, e + i * 32 * V, o, last);
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) load_rest<T, V>(next[i], grid, e + i * 32 * V, o, last);
+            }
+        };
+        fetch(0);
+        float most = minus_inf(), shift = 0.f;
+        Vals<4> s = all<4>(0.f), x2 = all<4>(0.f);
+        int b = 0;
+        for (int u = 0; u < units; ++u) {
+            float here_most = minus_inf();
+            for (const int end = min(batches, (u + 1) * unit); b < end;) {
+                Pack<T, V> raw[kBatch];
+                Largest<T, V> here;
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) { raw[i] = next[i]; here.take(raw[i]); }
+                if (++b < batches) fetch(b);
+                const float big = here.value();
+                here_most = fmaxf(here_most, big);
+                if (__any_sync(0xffffffffu, big > most)) {
+                    most = fmaxf(most, big);
+                    const float to = most == minus_inf() ? 0.f : most;
+                    // (a sum of 0 has no maximum yet, and one far below the new maximum counts for nothing: neither must make 0 * inf)
+                    const float d = sum_of(s) == 0.f ? 0.f : fmaxf((shift - to) * kLog2e, kLeast), f = ex2(d);
+                    x2 = mul(fma(s, all<4>(d), x2), all<4>(f));
+                    s = mul(s, all<4>(f));
+                    shift = to;
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    keep_packed(raw[i]);
+                    take_sums<kStats>(values(raw[i]), shift, s, x2);
+                }
+            }
+            if (a.top > 0) largest_of[warp][u][lane] = here_most;
+        }
+        const float m = lanes_max(most), to = m == minus_inf() ? 0.f : m;
+        Sums sums{to, sum_of(s), sum_of(x2)};
+        {
+            const float d = sums.s == 0.f ? 0.f : fmaxf((shift - to) * kLog2e, kLeast), f = ex2(d);
+            sums.t = lanes_sum(fmaf(sums.s, d, sums.t) * f);
+            sums.s = lanes_sum(sums.s * f);
+        }
+        const RowResult r = result_of(sums);
+        if (lane == 0) write_stats(a, row, r, label);
+        if (a.top == 0) continue;
+        if (lane == 0) *count = 0;
+        __syncwarp();
+        const float bound = bound_of(most, a.top);
+        for (int u = 0; u < units; ++u) {
+            for (unsigned who = __ballot_sync(0xffffffffu, largest_of[warp][u][lane] >= bound); who; who &= who - 1) {
+                const int first = (__ffs(who) - 1) * V, end = min(batches, (u + 1) * unit);
+                // a batch has 32 values of each lane (16 in fp32): one for each lane to look at
+                for (int at = u * unit; at < end; ++at) {
+                    const int e = at * kWide + (lane / V % kBatch) * 32 * V + first + lane % V;
+                    if (lane >= V * kBatch || e < o || e >= last) continue;
+                    const float v = fmaxf(to_f(grid[e]), minus_inf());
+                    if (v >= bound) {
+                        const int place = atomicAdd(count, 1);
+                        if (place < kListWarp) list[place] = key_of(v, e - o);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        __syncwarp();
+        const int found = best_of_list<T>(a, zr, *count, list, lane);
+        place(list, found, a.top, lane, 32, [&](int at, unsigned long long k) {
+            if (a.top_logp) a.top_logp[row * a.top + at] = logp_of(r, value_of(k));
+            if (a.top_index) a.top_index[row * a.top + at] = class_of(k);
+        });
+        __syncwarp();
     }
 }
 
@@ -465,7 +584,7 @@ logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_v
         const float m = lanes_max(part_max), shift = m == minus_inf() ? 0.f : m;
         Vals<V> s = all<V>(0.f), x2 = all<V>(0.f);
 #pragma unroll 4
-        for (int k = 0; k < vectors; ++k) take_sums<MODE, V>(values(load_pack<T, V>(mine_at + k * kStep)), shift, s, x2);
+        for (int k = 0; k < vectors; ++k) take_sums<MODE>(values(load_pack<T, V>(mine_at + k * kStep)), shift, s, x2);
         Sums sums{shift, lanes_sum(sum_of(s)), 0.f};
         if (MODE == kStats) sums.t = lanes_sum(sum_of(x2));
         if (lane == 0) sh.sums[turn][t >> 5] = sums;
@@ -485,7 +604,7 @@ logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_v
                     const int e = first + t * V + k * kStep;
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float v = fmaxf(to_f(p.v[j]), minus_inf());
+                        const float v = fmaxf(to_f(p.get(j)), minus_inf());
                         if (v >= bound && e + j >= o && e + j < last) {
                             const int at = atomicAdd(&sh.count[turn], 1);
                             if (at < kListBlock) sh.list[at] = key_of(v, e + j - o);
@@ -556,7 +675,7 @@ logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_v
                     else {
 #pragma unroll
                         for (int j = 0; j < V; ++j)
-                            if (e + j >= o && e + j < last) dr[e + j] = d.v[j];
+                            if (e + j >= o && e + j < last) dr[e + j] = d.get(j);
                     }
                 }
             }
@@ -684,7 +803,7 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
         for (int k = 0; k < a.top; ++k) {
             unsigned long long best = 0;
             each([&](const Pack<T, V>& q, int i) {
-                const unsigned long long key = key_of(to_f(q.v[0]), first + i);
+                const unsigned long long key = key_of(to_f(q.get(0)), first + i);
                 if (key < before && key > best) best = key;
             });
             before = across_warps(best, share, keys[k & 1], [](unsigned long long x, unsigned long long y) { return x > y ? x : y; });
@@ -738,10 +857,8 @@ __global__ void __launch_bounds__(32 * kMapWarps) logprob_map_kernel(LpArgs a, i
         const float k = labelled_rows(a);
         over = k > 0.f ? a.scale / k : 0.f;
     }
-    for (long long tile = (long long)blockIdx.x * groups + warp / share; tile < a.n * tiles; tile += (long long)gridDim.x * groups) {
-        const long long n = tile / tiles;
-        const int px0 = (int)(tile - n * tiles) * 32 * V;
-        logprob_tile<T, V, CPT, MODE, TOP>(a, n, px0 + lane * V, first, per, share, over, total, red, keys);
+    for (Walk w(blockIdx.x * groups + warp / share, gridDim.x * groups, tiles); w.hi < a.n; w.advance()) {
+        logprob_tile<T, V, CPT, MODE, TOP>(a, w.hi, w.lo * 32 * V + lane * V, first, per, share, over, total, red, keys);
         if (TOP && share > 1) __syncthreads();                  // (the keys' two buffers start over)
     }
     if (MODE == kLoss && a.sums) {
@@ -823,9 +940,9 @@ template <class T, int V, bool SHIFT> __global__ void __launch_bounds__(256) log
     previous_launches();
     constexpr int kPer = 4, kSegment = 32 * V * kPer;
     const int lane = threadIdx.x & 31;
-    for (long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); task < a.rows * segments; task += (long long)gridDim.x * 8) {
-        const long long row = segments == 1 ? task : task / segments;
-        const int first = (int)(task - row * segments) * kSegment + lane * V;
+    for (Walk w(blockIdx.x * 8 + (threadIdx.x >> 5), gridDim.x * 8, segments); w.hi < a.rows; w.advance()) {
+        const long long row = w.hi;
+        const int first = w.lo * kSegment + lane * V;
         const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
         const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0;
         const int hi = o + a.c;
@@ -858,15 +975,15 @@ template <class T, int V, bool SHIFT> __global__ void __launch_bounds__(256) log
     }
 }
 
-template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map_kernel(LpArgs a, int tiles, int slabs)
+template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map_kernel(LpArgs a, int tiles)
 {
     previous_launches();
     constexpr int kSlab = 16, kAhead = 8;
     const int lane = threadIdx.x & 31;
-    for (long long task = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); task < a.n * tiles * slabs; task += (long long)gridDim.x * 8) {
-        const long long at = task / slabs, n = at / tiles;
-        const int c0 = (int)(task - at * slabs) * kSlab, c1 = min(a.c, c0 + kSlab);
-        const int px = (int)(at - n * tiles) * 32 * V + lane * V;
+    const int c0 = blockIdx.y * kSlab, c1 = min(a.c, c0 + kSlab);
+    for (Walk w(blockIdx.x * 8 + (threadIdx.x >> 5), gridDim.x * 8, tiles); w.hi < a.n; w.advance()) {
+        const long long n = w.hi;
+        const int px = w.lo * 32 * V + lane * V;
         if (px >= a.p) continue;
         const T* zt = static_cast<const T*>(a.z) + n * a.z_stride + px;
         T* dt = static_cast<T*>(a.dz) + n * a.dz_stride + px;
@@ -943,6 +1060,16 @@ template <class T, bool SHIFT, int MODE> int pick_block_rows(const LpArgs& a, bo
     while (share() * 16 > kStageMost) cluster *= 2;
     while (cluster < 16 && a.rows * cluster * 2 <= kSms && share() > 512) cluster *= 2;
     constexpr bool kFin = MODE == kStats;
+    if constexpr (MODE == kStats) {
+        // a warp a row from 12 rows an SM on: 50 KB of loads on their way there
+        if (a.rows >= 12 * kSms) {
+            const int fit = resident<logprob_stream_rows_kernel<T, SHIFT>>(kStreamWarps * 32, 0);
+            const long long want = (a.rows + kStreamWarps - 1) / kStreamWarps, most = (long long)kSms * fit;
+            *blocks = (int)(want < most ? want : most);
+            launch(logprob_stream_rows_kernel<T, SHIFT>, dim3(*blocks), dim3(kStreamWarps * 32), 0, LaunchStream{st, true}, a);
+            return launched();
+        }
+    }
     if (cluster > 1) return run_block_rows<T, SHIFT, MODE, 512, false>(a, cluster, share(), dz_vec, blocks, st);
     if (share() <= 1024) return run_block_rows<T, SHIFT, MODE, 128, kFin>(a, 1, share(), dz_vec, blocks, st);
     return run_block_rows<T, SHIFT, MODE, 512, kFin>(a, 1, share(), dz_vec, blocks, st);
@@ -1021,8 +1148,8 @@ template <class T, int V, bool SHIFT> int bwd_rows(const LpArgs& a, LaunchStream
 template <class T, int V> int bwd_map(const LpArgs& a, LaunchStream ls)
 {
     const long long tiles = (a.p + 32 * V - 1) / (32 * V), slabs = (a.c + 15) / 16;
-    const long long want = (a.n * tiles * slabs + 7) / 8, most = 8LL * kSms;
-    launch(logprob_bwd_map_kernel<T, V>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, ls, a, (int)tiles, (int)slabs);
+    const long long want = (a.n * tiles + 7) / 8, most = (8LL * kSms + slabs - 1) / slabs;
+    launch(logprob_bwd_map_kernel<T, V>, dim3((unsigned)(want < most ? want : most), (unsigned)slabs), dim3(256), 0, ls, a, (int)tiles);
     return launched();
 }
 template <class T> int backward(const LpArgs& a, LaunchStream ls)

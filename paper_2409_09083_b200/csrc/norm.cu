@@ -86,8 +86,7 @@ template <class T, int V> struct Raw<T, V, true> {
     __device__ __forceinline__ void clear()
     {
         e = 1;
-#pragma unroll
-        for (int j = 0; j < V; ++j) q.v[j] = 0;
+        q = zero_pack<unsigned char, V>();
     }
     __device__ __forceinline__ Vals<V> hats(float rstd, float shift) const { return fma(steps_of(q), all<V>(rstd * step_of(e)), all<V>(shift)); }
     __device__ __forceinline__ Vals<V> hats(const Vals<V>& rstd, const Vals<V>& shift) const { return fma(steps_of(q), mul(rstd, all<V>(step_of(e))), shift); }
@@ -226,16 +225,16 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
         const int end = (a.c + kBlock - 1) / kBlock * kBlock;         // whole warps, for the blocks of a checkpoint
         for (int e = threadIdx.x; e < end; e += 1024) {
             Pack<T, 1> v = zero_pack<T, 1>();
-            if (e < a.c) v.v[0] = xr[e];
+            if (e < a.c) v.set(0, xr[e]);
             if (CK) {
                 const float big = largest(values(v));
                 unsigned ex = step_exponent(big);
                 const Pack<unsigned char, 1> st = special<T>(big) ? to_steps_special<T, 1>(values(v), ex) : to_steps(values(v), ex);
-                a.ck.q[row * a.ck.pitch + e] = st.v[0];
+                a.ck.q[row * a.ck.pitch + e] = st.get(0);
                 if (e % kBlock == 0) a.ck.steps[row * a.ck.blocks + e / kBlock] = (unsigned char)ex;
             }
             if (e < a.c)
-                yr[e] = from_f<T>(fmaf((to_f(v.v[0]) - mean) * rstd, a.weight ? a.weight[e] : 1.f, a.bias ? a.bias[e] : 0.f));
+                yr[e] = from_f<T>(fmaf((to_f(v.get(0)) - mean) * rstd, a.weight ? a.weight[e] : 1.f, a.bias ? a.bias[e] : 0.f));
         }
     }
 }
@@ -392,8 +391,8 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_lon
         const float shift = -mean * rstd;
         auto hat_of = [&](int e) {
             Raw<T, 1, CK> r;
-            if constexpr (CK) { r.q.v[0] = qr[e]; r.e = er[e / kBlock]; }
-            else r.a.v[0] = xr[e];
+            if constexpr (CK) { r.q.w[0] = qr[e]; r.e = er[e / kBlock]; }
+            else r.a.w[0] = bits_of(xr[e]);
             return r.hats(rstd, shift).v[0];
         };
         float s[2] = {0.f, 0.f};
@@ -424,11 +423,11 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_lon
 // warps of a block take a tile each and need no barrier.
 struct Tile { long long n, row; int px, first, count; bool live; };
 
-__device__ __forceinline__ Tile tile_of(const NormArgs& a, long long tile, int tiles, int pixels, int at, int first, int per)
+__device__ __forceinline__ Tile tile_of(const NormArgs& a, const Walk& w, int pixels, int at, int first, int per)
 {
     Tile t;
-    t.n = tile / tiles;
-    t.px = (int)(tile - t.n * tiles) * pixels + at;
+    t.n = w.hi;
+    t.px = w.lo * pixels + at;
     t.live = t.px < a.p;
     t.row = t.n * a.p + t.px;
     t.first = first;
@@ -555,8 +554,8 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 3 : 1) norm_fwd_map_kernel
     float* red = smem + 2 * a.c;
     stage_cols(a, wb);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = warp / share, groups = (blockDim.x >> 5) / share;
-    for (long long tile = (long long)blockIdx.x * groups + group; tile < a.n * tiles; tile += (long long)gridDim.x * groups) {
-        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, (warp & (share - 1)) * per, per);
+    for (Walk w(blockIdx.x * groups + group, gridDim.x * groups, tiles); w.hi < a.n; w.advance()) {
+        const Tile t = tile_of(a, w, 32 * V, lane * V, (warp & (share - 1)) * per, per);
         if (t.count == CPT && t.px - lane * V + 32 * V <= a.p) norm_fwd_tile<T, V, CPT, CK, true>(a, t, share, red, blockDim.x * V, wb);
         else norm_fwd_tile<T, V, CPT, CK, false>(a, t, share, red, blockDim.x * V, wb);
     }
@@ -568,8 +567,8 @@ template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_f
     __shared__ float red[2][512 * V];
     previous_launches();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    for (long long tile = blockIdx.x; tile < a.n * tiles; tile += gridDim.x) {
-        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, 0, a.c);
+    for (Walk w(blockIdx.x, gridDim.x, tiles); w.hi < a.n; w.advance()) {
+        const Tile t = tile_of(a, w, 32 * V, lane * V, 0, a.c);
         const T* xt = static_cast<const T*>(a.x) + t.n * a.x_stride + t.px;
         T* yt = static_cast<T*>(a.out) + t.n * a.out_stride + t.px;
         auto load = [&](int ch) { return t.live ? values(load_pack<T, V>(xt + (long long)ch * a.p)) : all<V>(0.f); };
@@ -638,8 +637,7 @@ __device__ __forceinline__ void load_map(const NormArgs& a, const Tile& t, int c
     dy = zero_pack<T, V>();
     if constexpr (CK) {
         x.e = 1;
-#pragma unroll
-        for (int j = 0; j < V; ++j) x.q.v[j] = 0;
+        x.q = zero_pack<unsigned char, V>();
     } else x.a = zero_pack<T, V>();
     if (!t.live) return;
     dy = load_pack<T, V>(static_cast<const T*>(a.dy) + t.n * a.dy_stride + at);
@@ -736,8 +734,8 @@ __global__ void __launch_bounds__(512) norm_bwd_map_kernel(NormArgs a, int share
 #pragma unroll
     for (int i = 0; i < ChannelSums<CPT>::kRegs; ++i) cs.dw[i] = cs.db[i] = 0.f;
     int turn = 0;
-    for (long long tile = (long long)blockIdx.x * groups + group; tile < a.n * tiles; tile += (long long)gridDim.x * groups, turn ^= 1) {
-        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, (warp & (share - 1)) * per, per);
+    for (Walk w(blockIdx.x * groups + group, gridDim.x * groups, tiles); w.hi < a.n; w.advance(), turn ^= 1) {
+        const Tile t = tile_of(a, w, 32 * V, lane * V, (warp & (share - 1)) * per, per);
         if (t.count == CPT && t.px - lane * V + 32 * V <= a.p)
             norm_bwd_tile<T, V, CPT, CK, true>(a, t, share, red + turn * half, wb, cs);
         else
@@ -771,8 +769,9 @@ template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_b
     const float inv_c = 1.f / (float)a.c;
     float* set = a.partials ? a.partials + (long long)blockIdx.x * 2 * a.c : nullptr;
     int turn = 0;
-    for (long long tile = blockIdx.x; tile < a.n * tiles; tile += gridDim.x, turn ^= 1) {
-        const Tile t = tile_of(a, tile, tiles, 32 * V, lane * V, 0, a.c);
+    bool first = true;
+    for (Walk w(blockIdx.x, gridDim.x, tiles); w.hi < a.n; w.advance(), turn ^= 1, first = false) {
+        const Tile t = tile_of(a, w, 32 * V, lane * V, 0, a.c);
         Vals<V> rstd, shift, s[2] = {all<V>(0.f), all<V>(0.f)};
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -781,7 +780,6 @@ template <class T, int V, bool CK> __global__ void __launch_bounds__(512) norm_b
         }
         Raw<T, V, CK> x;
         Pack<T, V> dy;
-        const bool first = tile == blockIdx.x;
         for (int ch = warp; ch < a.c; ch += warps) {
             load_map<T, V, CK>(a, t, ch, x, dy);
             const float w = a.weight ? __ldg(a.weight + ch) : 1.f;
