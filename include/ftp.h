@@ -471,7 +471,8 @@ int ftp_plan_wait_probe(ftp_plan* plan, void* workspace, int limit_us, void* str
  * Arrays are DEVICE memory of the type in ftp_dims, each sample dense; `..._stride` is the number of elements from one sample to
  * the next (0: dense; else at least c p).  Any alignment that the type itself allows is accepted; 16-byte aligned arrays and strides
  * are the fast ones.  An output array may be the input array it is computed from where the entry says so; otherwise arrays do not
- * overlap.  Elements between samples are neither read nor written.  Sums, statistics and probabilities are held in fp32; results
+ * overlap.  Elements between samples are not written
+ * and what they hold is of no account.  Sums, statistics and probabilities are held in fp32; results
  * of 16 bits are rounded once, to nearest.  Sums are taken in a fixed order: the same call gives the same bits.
  *
  * None of these calls allocates, synchronises, needs a plan or keeps anything between calls, and all can be captured in a CUDA

@@ -92,10 +92,30 @@ template <class T, int V> __device__ __forceinline__ void keep_packed(Pack<T, V>
     }
 }
 
-// Values [e, e + V) of an array of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as `fill`
-// and is not written.  Loads come in two steps: load_whole of all a thread's words, each one predicated instruction, then load_rest
-// where a word lies across an end.  (One function with both would put a branch between any two loads, and the next would not be
-// issued before the last has arrived.)  Places are ints, relative to the row or segment: wide ones cost more than the arithmetic.
+// Values [e, e + V) of a row of which only [lo, hi) exist, `base` aligned for whole words; what does not exist reads as `fill` and is
+// not written.  Words that lie across an end of the row come in three steps, so that no branch stands between any two loads and none is
+// waited for before it is used: load_whole of all a thread's words, each one predicated instruction, with the bounds that reach()
+// widens where the neighbouring memory is the array's too; load_rest, value by value, for the first and last rows, where it is not;
+// and keep_part, where the values are used, which puts `fill` in the places that are not the row's.  Places are ints, relative to the
+// row or segment: wide ones cost more than the arithmetic.
+template <class T, int V> struct Reach {
+    int lo, hi;          // of load_whole
+    bool all;            // nothing is left to load_rest
+};
+// `row`: first value of the row, `count` values; [begin, end) the array, from its first value to its last.
+template <class T, int V> __device__ __forceinline__ Reach<T, V> reach(const T* row, int lo, int hi, const T* begin, const T* end)
+{
+    const bool before = row - begin >= V, behind = end - (row + (hi - lo)) >= V;
+    return {before ? lo - (V - 1) : lo, behind ? hi + V - 1 : hi, before && behind};
+}
+template <class T, int V> __device__ __forceinline__ void keep_part(Pack<T, V>& r, int e, int lo, int hi, T fill)
+{
+    if (V > 1 && (e < lo || e + V > hi)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (e + j < lo || e + j >= hi) r.set(j, fill);
+    }
+}
 template <class T, int V> __device__ __forceinline__ Pack<T, V> filled(T fill)
 {
     Pack<T, V> r;
@@ -122,6 +142,36 @@ template <class T, int V> __device__ __forceinline__ void store_part(T* base, in
 #pragma unroll
     for (int j = 0; j < V; ++j)
         if (e + j >= lo && e + j < hi) base[e + j] = a.get(j);
+}
+
+// Values [o, o + V) of the 2 V in `lo` and `hi`, 0 <= o < V: a vector that lies across two words of the grid.
+template <class T, int V> __device__ __forceinline__ Pack<T, V> window(const Pack<T, V>& lo, const Pack<T, V>& hi, int o)
+{
+    constexpr int N = Pack<T, V>::kWords;
+    static_assert(sizeof(T) * V >= 4, "whole words");
+    const unsigned bytes = (unsigned)o * sizeof(T), bits = (bytes & 3u) * 8u;
+    unsigned w[2 * N + 1];
+#pragma unroll
+    for (int j = 0; j < N; ++j) { w[j] = lo.w[j]; w[N + j] = hi.w[j]; }
+    w[2 * N] = 0u;
+#pragma unroll
+    for (int d = 1; d < N; d <<= 1) {
+        const bool move = (bytes >> 2) & d;
+#pragma unroll
+        for (int j = 0; j + d <= 2 * N; ++j) w[j] = move ? w[j + d] : w[j];
+    }
+    Pack<T, V> r;
+#pragma unroll
+    for (int j = 0; j < N; ++j) r.w[j] = __funnelshift_r(w[j], w[j + 1], bits);
+    return r;
+}
+// The pack of the next lane.
+template <class T, int V> __device__ __forceinline__ Pack<T, V> from_next_lane(const Pack<T, V>& a)
+{
+    Pack<T, V> r;
+#pragma unroll
+    for (int j = 0; j < Pack<T, V>::kWords; ++j) r.w[j] = __shfl_down_sync(0xffffffffu, a.w[j], 1);
+    return r;
 }
 
 // V values as fp32, in pairs where V is even: the packed fp32 instructions of sm_100 do two values in one issue slot, and all of
@@ -377,6 +427,33 @@ template <int V> __device__ __forceinline__ Vals<V> steps_of(const Pack<unsigned
     }
     return r;
 }
+
+// Steps of columns [col, col + V) of a run, col a multiple of V less o (0 < o < V): they lie across two words of the run and, it may be,
+// across two blocks.  Columns before the run or behind its padding are 0.
+template <int V> struct ShiftedSteps {
+    Pack<unsigned char, V> lo, hi;
+    unsigned e0, e1;
+    __device__ __forceinline__ void load(const unsigned char* q, const unsigned char* steps, int col, int o, int padded)
+    {
+        const int at = col + o;
+        lo = hi = zero_pack<unsigned char, V>();
+        if (at >= V && at - V < padded) lo = load_pack<unsigned char, V>(q + at - V);
+        if (at < padded) hi = load_pack<unsigned char, V>(q + at);
+        e0 = steps[max(0, min(col, padded - 1)) / kBlock];
+        e1 = steps[min(max(0, col + V - 1), padded - 1) / kBlock];
+    }
+    // the numbers of steps, and each one's step times `by`
+    __device__ __forceinline__ Vals<V> numbers(int o) const { return steps_of(window<unsigned char, V>(lo, hi, V - o)); }
+    __device__ __forceinline__ Vals<V> scales(int col, float by) const
+    {
+        const float s0 = step_of(e0) * by, s1 = step_of(e1) * by;
+        const int second = (col + V - 1) & ~(kBlock - 1);            // first column of the block that the last one is in
+        Vals<V> r;
+#pragma unroll
+        for (int j = 0; j < V; ++j) r.v[j] = col + j >= second ? s1 : s0;
+        return r;
+    }
+};
 
 // Where a checkpoint lies: q bytes of run r (a row or plane of `len` values) at r * pitch, its step bytes at steps + r * blocks.
 struct CkptView {

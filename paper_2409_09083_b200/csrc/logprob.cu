@@ -283,16 +283,21 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
         const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
         const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0, last = o + a.c;
         Pack<T, V> raw[NV];
+        const Reach<T, V> in = reach<T, V>(zr, o, last, static_cast<const T*>(a.z), static_cast<const T*>(a.z) + (a.rows - 1) * a.z_stride + a.c);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             raw[i] = filled<T, V>(from_f<T>(minus_inf()));
-            load_whole<T, V>(raw[i], zr - o, (i * 32 + lane) * V, o, last);
+            load_whole<T, V>(raw[i], zr - o, (i * 32 + lane) * V, in.lo, in.hi);
         }
         Label label{-1, 0.f, 0};
         if (MODE == kLoss || lane == 0) label = read_label<T>(a, row, zr, 1);
         if (SHIFT || a.c % V) {
+            if (!in.all) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) load_rest<T, V>(raw[i], zr - o, (i * 32 + lane) * V, o, last);
+                for (int i = 0; i < NV; ++i) load_rest<T, V>(raw[i], zr - o, (i * 32 + lane) * V, o, last);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) keep_part<T, V>(raw[i], (i * 32 + lane) * V, o, last, from_f<T>(minus_inf()));
         }
         Largest<T, V> most;
 #pragma unroll
@@ -946,16 +951,17 @@ template <class T, int V, bool SHIFT> __global__ void __launch_bounds__(256) log
         const T* zr = static_cast<const T*>(a.z) + row * a.z_stride;
         const int o = SHIFT ? (int)((reinterpret_cast<uintptr_t>(zr) / sizeof(T)) & (V - 1)) : 0;
         const int hi = o + a.c;
+        const Reach<T, V> in = reach<T, V>(zr, o, hi, static_cast<const T*>(a.z), static_cast<const T*>(a.z) + (a.rows - 1) * a.z_stride + a.c);
         zr -= o;
         T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
         Pack<T, V> raw[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             raw[i] = zero_pack<T, V>();
-            load_whole<T, V>(raw[i], zr, first + i * 32 * V, o, hi);
+            load_whole<T, V>(raw[i], zr, first + i * 32 * V, in.lo, in.hi);          // (places outside the row are not stored: they may hold anything)
         }
         const RowGrad r = row_grad(a, row);
-        if (SHIFT || a.c % V) {
+        if ((SHIFT || a.c % V) && !in.all) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) load_rest<T, V>(raw[i], zr, first + i * 32 * V, o, hi);
         }

@@ -105,16 +105,20 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
 {
     constexpr bool kWhole = FORM == kFast || V == 1;
     __shared__ float red[2][16];
+    constexpr bool kEdges = CK && FORM == kShift;
+    __shared__ __align__(16) Pack<T, V> edge[kEdges ? 2 : 1][kEdges ? 16 : 1][kEdges ? VPT : 1];       // first vectors of the warps, of this row and the one before
+    int turn = 0;
     previous_launches();
     const int per = tpr > 32 ? 1 : blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = tpr > 32 ? 0 : threadIdx.x / tpr;
     const float inv_c = 1.f / (float)a.c;
     const long long step = (long long)gridDim.x * per;
-    for (long long row0 = (long long)blockIdx.x * per; row0 < a.rows; row0 += step) {
+    for (long long row0 = (long long)blockIdx.x * per; row0 < a.rows; row0 += step, turn ^= 1) {
         const long long row = row0 + group;
         const bool live = row < a.rows;
         const T* xr = static_cast<const T*>(a.x) + row * a.x_stride;
         const int o = FORM == kShift ? (int)((reinterpret_cast<uintptr_t>(xr) / sizeof(T)) & (V - 1)) : 0;
         const int hi = live ? o + a.c : 0;
+        const Reach<T, V> in = reach<T, V>(xr, o, o + a.c, static_cast<const T*>(a.x), static_cast<const T*>(a.x) + (a.rows - 1) * a.x_stride + a.c);
         xr += t * V - o;
         Pack<T, V> raw[VPT];
 #pragma unroll
@@ -122,11 +126,22 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
             const int e = (i * tpr + t) * V;
             raw[i] = zero_pack<T, V>();
             if (kWhole) { if (e < hi) raw[i] = load_pack<T, V>(xr + i * tpr * V); }
-            else load_whole<T, V>(raw[i], xr - t * V, e, o, hi);
+            else if (live) load_whole<T, V>(raw[i], xr - t * V, e, in.lo, in.hi);
         }
-        if (!kWhole) {
+        if (!kWhole && live) {
+            if (!in.all) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) load_rest<T, V>(raw[i], xr - t * V, (i * tpr + t) * V, o, hi);
+                for (int i = 0; i < VPT; ++i) load_rest<T, V>(raw[i], xr - t * V, (i * tpr + t) * V, o, hi);
+            }
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) keep_part<T, V>(raw[i], (i * tpr + t) * V, o, hi, from_f<T>(0.f));
+        }
+        if constexpr (kEdges) {                                 // (read behind the barriers, or the warp's exchanges, of the sums)
+            if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) edge[turn][threadIdx.x >> 5][i] = raw[i];
+            }
+            __syncwarp();
         }
         Vals<V> acc = values(raw[0]);
 #pragma unroll
@@ -160,45 +175,66 @@ __global__ void __launch_bounds__(MOST, MOST > 128 ? 1 : 6) norm_fwd_rows_kernel
         T* yr = static_cast<T*>(a.out) + row * a.out_stride + t * V - o;
         unsigned char* qr = a.ck.q + row * a.ck.pitch + t * V;
         unsigned char* er = a.ck.steps + row * a.ck.blocks + t * V / kBlock;
-        bool any = false;
+        // The checkpoint first, before y may have been written over x: columns [e, e + V) of the row are places o further on, across a vector
+        // of this lane and of the next one, which for the last lane of a warp lies in shared memory.
+        if constexpr (CK) {
+            auto columns = [&](const Pack<T, V>& mine, int i) {
+                if constexpr (FORM == kShift) {
+                    Pack<T, V> next = from_next_lane(mine);
+                    if ((t & 31) == 31 || t == tpr - 1) {
+                        const int w = (t >> 5) + 1, warps = tpr >> 5;          // (the last warp goes on with the first one's next vector)
+                        next = zero_pack<T, V>();
+                        if (w < warps) next = edge[turn][w][i];
+                        else if (i + 1 < VPT && warps > 0) next = edge[turn][tpr > 32 ? 0 : threadIdx.x >> 5][(i + 1) % VPT];
+                    }
+                    return values(window<T, V>(mine, next, o));
+                } else return values(mine);
+            };
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {                         // as if all values were finite
+                const int skip = i * tpr * V;
+                const Vals<V> k = columns(raw[i], i);
+                const float big = largest(k);
+                any |= special<T>(big);
+                const unsigned ex = step_exponent(big);
+                if (live && skip + t * V < a.ck.pitch) {
+                    store_pack<unsigned char, V>(qr + skip, to_steps(k, ex));
+                    if (t % (kBlock / V) == 0) er[(unsigned)skip / kBlock] = (unsigned char)ex;
+                }
+            }
+            if (__any_sync(0xffffffffu, any)) {                     // the blocks with others once more
+#pragma unroll 1
+                for (int i = 0; i < VPT; ++i) {
+                    const int skip = i * tpr * V, e = skip + t * V;
+                    Pack<T, V> again = zero_pack<T, V>();
+                    load_whole<T, V>(again, xr - t * V, e, o, hi);
+                    load_rest<T, V>(again, xr - t * V, e, o, hi);
+                    const Vals<V> k = columns(again, i);
+                    if (special<T>(largest(k))) {
+                        unsigned ex;
+                        const Pack<unsigned char, V> st = to_steps_special<T, V>(k, ex);
+                        if (live && e < a.ck.pitch) {
+                            store_pack<unsigned char, V>(qr + skip, st);
+                            if (t % (kBlock / V) == 0) er[(unsigned)skip / kBlock] = (unsigned char)ex;
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) keep_packed(raw[i]);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int skip = i * tpr * V, e = skip + t * V;
-            const Vals<V> v = values(raw[i]);
-            if (CK) {                                           // as if all values were finite
-                const float big = largest(v);
-                any |= special<T>(big);
-                const unsigned ex = step_exponent(big);
-                if (live && e < a.ck.pitch) {
-                    store_pack<unsigned char, V>(qr + skip, to_steps(v, ex));
-                    if (t % (kBlock / V) == 0) er[(unsigned)skip / kBlock] = (unsigned char)ex;
-                }
-            }
-            if (e < hi) {
-                Vals<V> w, b;
-                load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v);
-                load_cols<FORM == kFast, V>(a.bias, e - o, a.c, 0.f, b.v);
-                const Pack<T, V> y = rounded<T, V>(fma(mul(add(v, all<V>(-mean)), all<V>(rstd)), w, b));
-                if (kWhole) store_pack<T, V>(yr + skip, y);
-                else store_part<T, V>(yr - t * V, e, o, hi, y);
-            }
-        }
-        if (CK && __any_sync(0xffffffffu, any)) {               // the blocks with others once more
-#pragma unroll 1
-            for (int i = 0; i < VPT; ++i) {
-                const int skip = i * tpr * V, e = skip + t * V;
-                Pack<T, V> again = zero_pack<T, V>();
-                load_whole<T, V>(again, xr - t * V, e, 0, hi);
-                load_rest<T, V>(again, xr - t * V, e, 0, hi);
-                const Vals<V> v = values(again);
-                if (!special<T>(largest(v))) continue;
-                unsigned ex;
-                const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
-                if (live && e < a.ck.pitch) {
-                    store_pack<unsigned char, V>(qr + skip, st);
-                    if (t % (kBlock / V) == 0) er[(unsigned)skip / kBlock] = (unsigned char)ex;
-                }
-            }
+            if (e >= hi) continue;
+            Vals<V> w, b;
+            load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v);
+            load_cols<FORM == kFast, V>(a.bias, e - o, a.c, 0.f, b.v);
+            const Pack<T, V> y = rounded<T, V>(fma(mul(add(values(raw[i]), all<V>(-mean)), all<V>(rstd)), w, b));
+            if (kWhole) store_pack<T, V>(yr + skip, y);
+            else store_part<T, V>(yr - t * V, e, o, hi, y);
         }
     }
 }
@@ -241,60 +277,87 @@ template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_fwd_lon
 
 // Backward pass of matrices; the same spread of a row over a group, a block's groups (each with a barrier of its own) taking rows in
 // turn.  A thread's columns are the same in every row, so dweight and dbias of its columns add up in registers over all rows of the block.
+// SHIFT keeps that true for rows off the 16-byte grid: a group's rows are a multiple of V rows apart, so that all of them start the
+// same distance o behind the grid, and place e is column e - o in each.
 // The next row's values are on their way while a row is summed: with one block of 512 threads an SM, whose 128 registers a thread hold the
 // sums, 32 KB are always in flight.
-template <class T, int V, int VPT, bool CK> struct RowIn {
-    Raw<T, V, CK> x[VPT];
+template <class T, int V, bool SHIFT, bool CK> struct RowX {
+    Raw<T, V, CK> raw;
+    __device__ __forceinline__ Vals<V> hats(float rstd, float shift, int, int) const { return raw.hats(rstd, shift); }
+};
+template <class T, int V> struct RowX<T, V, true, true> {
+    ShiftedSteps<V> steps;
+    Raw<T, V, true> raw;                                 // where o = 0
+    __device__ __forceinline__ Vals<V> hats(float rstd, float shift, int e, int o) const
+    {
+        return o == 0 ? raw.hats(rstd, shift) : fma(steps.numbers(o), steps.scales(e - o, rstd), all<V>(shift));
+    }
+};
+template <class T, int V, int VPT, bool SHIFT, bool CK> struct RowIn {
+    RowX<T, V, SHIFT, CK> x[VPT];
     Pack<T, V> dy[VPT];
     float mean, rstd;
 };
-// Where a thread's first vector of a row lies; the others follow at multiples of tpr vectors.
+// Where a thread's first vector of a row lies; the others follow at multiples of tpr vectors.  (The checkpoint's: of the row itself.)
 template <class T> struct RowAt {
     const T *x, *dy;
     T* out;
     const unsigned char *q, *e;
     const float *mean, *rstd;
 };
-template <class T, int V, int VPT, bool FAST, bool CK>
-__device__ __forceinline__ void load_row(const RowAt<T>& at, bool live, int c, int tpr, int t, RowIn<T, V, VPT, CK>& in)
+template <class T, int V, int VPT, int FORM, bool CK>
+__device__ __forceinline__ void load_row(const NormArgs& a, const RowAt<T>& at, bool live, int o, int tpr, int t, RowIn<T, V, VPT, FORM == kShift, CK>& in)
 {
-    constexpr bool kWhole = FAST || V == 1;
+    constexpr bool kWhole = FORM == kFast || V == 1;
+    const int hi = o + a.c;
+    Reach<T, V> rd{o, hi, true}, rx{o, hi, true};
+    if (!kWhole && live) {
+        rd = reach<T, V>(at.dy - t * V + o, o, hi, static_cast<const T*>(a.dy), static_cast<const T*>(a.dy) + (a.rows - 1) * a.dy_stride + a.c);
+        if constexpr (!CK) rx = reach<T, V>(at.x - t * V + o, o, hi, static_cast<const T*>(a.x), static_cast<const T*>(a.x) + (a.rows - 1) * a.x_stride + a.c);
+    }
     in.mean = in.rstd = 0.f;
     if (live) { in.mean = *at.mean; in.rstd = *at.rstd; }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int skip = i * tpr * V, e = skip + t * V;
         in.dy[i] = zero_pack<T, V>();
-        in.x[i].clear();
-        if (live && e < c) {
+        in.x[i].raw.clear();
+        if (live && e < hi) {
             if (kWhole) in.dy[i] = load_pack<T, V>(at.dy + skip);
-            else load_whole<T, V>(in.dy[i], at.dy - t * V, e, 0, c);
+            else load_whole<T, V>(in.dy[i], at.dy - t * V, e, rd.lo, rd.hi);
             if constexpr (CK) {
-                in.x[i].q = load_pack<unsigned char, V>(at.q + skip);
-                in.x[i].e = at.e[(unsigned)skip / kBlock];
+                if constexpr (FORM == kShift) {
+                    if (o > 0) { in.x[i].steps.load(at.q, at.e, e - o, o, (int)a.ck.pitch); continue; }
+                }
+                in.x[i].raw.q = load_pack<unsigned char, V>(at.q + e);
+                in.x[i].raw.e = at.e[(unsigned)e / kBlock];
             } else {
-                if (kWhole) in.x[i].a = load_pack<T, V>(at.x + skip);
-                else load_whole<T, V>(in.x[i].a, at.x - t * V, e, 0, c);
+                if (kWhole) in.x[i].raw.a = load_pack<T, V>(at.x + skip);
+                else load_whole<T, V>(in.x[i].raw.a, at.x - t * V, e, rx.lo, rx.hi);
             }
+        } else if constexpr (CK && FORM == kShift) {
+            in.x[i].steps.lo = in.x[i].steps.hi = zero_pack<unsigned char, V>();
+            in.x[i].steps.e0 = in.x[i].steps.e1 = 1;
         }
     }
-    if (!kWhole && live) {
+    if (!kWhole && live && !(rd.all && rx.all)) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            load_rest<T, V>(in.dy[i], at.dy - t * V, e, 0, c);
-            if constexpr (!CK) load_rest<T, V>(in.x[i].a, at.x - t * V, e, 0, c);
+            load_rest<T, V>(in.dy[i], at.dy - t * V, e, o, hi);
+            if constexpr (!CK) load_rest<T, V>(in.x[i].raw.a, at.x - t * V, e, o, hi);
         }
     }
 }
 
-template <class T, int V, int VPT, bool FAST, bool CK>
+template <class T, int V, int VPT, int FORM, bool CK>
 __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int tpr)
 {
-    constexpr bool kWhole = FAST || V == 1;
+    constexpr bool kWhole = FORM == kFast || V == 1;
     constexpr int E = V * VPT;
     extern __shared__ float smem[];                    // a set of columns per group, to add the groups of the block
     __shared__ float red[2][32];
+    __shared__ int shifts[64];
     previous_launches();
     next_launch();
     const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = threadIdx.x / tpr;
@@ -303,23 +366,33 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
     const long long step = (long long)gridDim.x * per;
     long long row = (long long)blockIdx.x * per + group;
     RowAt<T> at;
-    at.x = static_cast<const T*>(a.x) + row * a.x_stride + t * V;
-    at.dy = static_cast<const T*>(a.dy) + row * a.dy_stride + t * V;
-    at.out = static_cast<T*>(a.out) + row * a.out_stride + t * V;
-    at.q = a.ck.q + row * a.ck.pitch + t * V;
-    at.e = a.ck.steps + row * a.ck.blocks + t * V / kBlock;
+    at.dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
+    const int o = FORM == kShift ? (int)((reinterpret_cast<uintptr_t>(at.dy) / sizeof(T)) & (V - 1)) : 0;
+    const int hi = o + a.c;
+    at.dy += t * V - o;
+    at.x = static_cast<const T*>(a.x) + row * a.x_stride + t * V - o;
+    at.out = static_cast<T*>(a.out) + row * a.out_stride + t * V - o;
+    at.q = a.ck.q + row * a.ck.pitch;
+    at.e = a.ck.steps + row * a.ck.blocks;
     at.mean = a.mean + row;
     at.rstd = a.rstd + row;
-    RowIn<T, V, VPT, CK> next;
-    load_row<T, V, VPT, FAST, CK>(at, row < a.rows, a.c, tpr, t, next);
+    RowIn<T, V, VPT, FORM == kShift, CK> next;
+    load_row<T, V, VPT, FORM, CK>(a, at, row < a.rows, o, tpr, t, next);
     int turn = 0;
     // (groups narrower than a warp stay together: a warp goes on until none of its rows is left)
     for (long long first = (long long)blockIdx.x * per + (tpr < 32 ? (threadIdx.x & ~31) / tpr : group); first < a.rows; first += step, turn ^= 1) {
         const float rstd = next.rstd, shift = -next.mean * next.rstd;
+        if (!kWhole) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                keep_part<T, V>(next.dy[i], (i * tpr + t) * V, o, hi, from_f<T>(0.f));
+                if constexpr (!CK) keep_part<T, V>(next.x[i].raw.a, (i * tpr + t) * V, o, hi, from_f<T>(0.f));
+            }
+        }
         Vals<E> d, hat;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const Vals<V> di = values(next.dy[i]), hi = next.x[i].hats(rstd, shift);
+            const Vals<V> di = values(next.dy[i]), hi = next.x[i].hats(rstd, shift, (i * tpr + t) * V, o);
 #pragma unroll
             for (int j = 0; j < V; ++j) { d.v[i * V + j] = di.v[j]; hat.v[i * V + j] = hi.v[j]; }
         }
@@ -328,14 +401,14 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
         at.x += step * a.x_stride; at.dy += step * a.dy_stride;
         at.q += step * a.ck.pitch; at.e += step * a.ck.blocks;
         at.mean += step; at.rstd += step;
-        load_row<T, V, VPT, FAST, CK>(at, row < a.rows, a.c, tpr, t, next);
+        load_row<T, V, VPT, FORM, CK>(a, at, row < a.rows, o, tpr, t, next);
         dw = fma(d, hat, dw);
         db = add(db, d);
         Vals<E> w = all<E>(0.f);                       // (from L1: 16 registers more would spill)
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int e = (i * tpr + t) * V;
-            if (e < a.c) load_cols<FAST, V>(a.weight, e, a.c, 1.f, w.v + i * V);
+            if (e < hi) load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v + i * V);
         }
         const Vals<E> g = mul(d, w);
         float s[2] = {sum_of(g), sum_of(mul(g, hat))};
@@ -348,9 +421,9 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
                 Vals<V> v;
 #pragma unroll
                 for (int j = 0; j < V; ++j) v.v[j] = dx.v[i * V + j];
-                if (e < a.c) {
+                if (e < hi) {
                     if (kWhole) store_pack<T, V>(at.out + skip, rounded<T, V>(v));
-                    else store_part<T, V>(at.out - t * V, e, 0, a.c, rounded<T, V>(v));
+                    else store_part<T, V>(at.out - t * V, e, o, hi, rounded<T, V>(v));
                 }
             }
         }
@@ -359,6 +432,7 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
     if (!a.partials) return;
     const int width = tpr * E;
     float* set = a.partials + (long long)blockIdx.x * 2 * a.c;
+    if (t == 0) shifts[group] = o;
     for (int k = 0; k < 2; ++k) {
         __syncthreads();
 #pragma unroll
@@ -366,10 +440,10 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
 #pragma unroll
             for (int j = 0; j < V; ++j) smem[group * width + (i * tpr + t) * V + j] = k ? db.v[i * V + j] : dw.v[i * V + j];
         __syncthreads();
-        for (int e = threadIdx.x; e < a.c; e += blockDim.x) {
+        for (int col = threadIdx.x; col < a.c; col += blockDim.x) {
             float s = 0.f;
-            for (int g = 0; g < per; ++g) s += smem[g * width + e];
-            set[(long long)k * a.c + e] = s;
+            for (int g = 0; g < per; ++g) s += smem[g * width + col + shifts[g]];
+            set[(long long)k * a.c + col] = s;
         }
     }
 }
@@ -864,8 +938,7 @@ template <class T, bool CK> int fwd_rows(const NormArgs& a, LaunchStream ls)
     const bool same = ((reinterpret_cast<uintptr_t>(a.x) ^ reinterpret_cast<uintptr_t>(a.out)) & 15) == 0 &&
                       (one || (a.x_stride - a.out_stride) % V == 0);
     if (on_grid) return a.c % V == 0 && a.weight && a.bias && a.w_vec ? pick_fwd_rows<T, V, kFast, CK>(a, ls) : pick_fwd_rows<T, V, kEdge, CK>(a, ls);
-    if constexpr (!CK)
-        if (same) return pick_fwd_rows<T, V, kShift, false>(a, ls);
+    if (same) return pick_fwd_rows<T, V, kShift, CK>(a, ls);
     return pick_fwd_rows<T, 1, kEdge, CK>(a, ls);
 }
 
@@ -876,38 +949,45 @@ int sum_sets(const NormArgs& a, int sets, float* dweight, float* dbias, LaunchSt
     return launched();
 }
 
-template <class T, int V, int VPT, bool FAST, bool CK> int run_bwd_rows(const NormArgs& a, int tpr, float* dweight, float* dbias, LaunchStream ls)
+template <class T, int V, int VPT, int FORM, bool CK> int run_bwd_rows(const NormArgs& a, int tpr, float* dweight, float* dbias, LaunchStream ls)
 {
     const int per = 512 / tpr;
     const size_t smem = a.partials ? (size_t)512 * VPT * V * 4 : 0;
-    const int blocks = fewer((a.rows + per - 1) / per, kSms);
-    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FAST, CK>, smem)) return FTP_ERR_CUDA;
-    launch(norm_bwd_rows_kernel<T, V, VPT, FAST, CK>, dim3(blocks), dim3(512), smem, ls, a, tpr);
+    int blocks = fewer((a.rows + per - 1) / per, kSms);
+    // rows of a group a multiple of V rows apart (unless each has one row only)
+    if (FORM == kShift && (long long)blocks * per < a.rows && per < V) blocks -= blocks % (V / per);
+    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, smem)) return FTP_ERR_CUDA;
+    launch(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, dim3(blocks), dim3(512), smem, ls, a, tpr);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
-// 16 values to a thread; rows of up to 8192 columns.
-template <class T, int V, bool FAST, bool CK> int pick_bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
+// 16 values to a thread (8 in fp32, whose values as read take the registers of two); rows of up to 8192 columns.
+template <class T, int V, int FORM, bool CK> int pick_bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
-    const long long vecs = (a.c + V - 1) / V;
+    const long long vecs = (a.c + (FORM == kShift ? V - 1 : 0) + V - 1) / V;
     const int least = kBlock / V < 8 ? 8 : kBlock / V;
     auto group = [&](int vpt) { const int t = pow2_at_least((vecs + vpt - 1) / vpt); return t < least ? least : t; };
     constexpr int kWide = 16 / V;
-    if (vecs <= 32) return run_bwd_rows<T, V, 1, FAST, CK>(a, group(1), dweight, dbias, ls);
-    if (vecs <= kWide * 512) return run_bwd_rows<T, V, kWide, FAST, CK>(a, group(kWide), dweight, dbias, ls);
+    if (vecs <= 32) return run_bwd_rows<T, V, 1, FORM, CK>(a, group(1), dweight, dbias, ls);
+    if constexpr (sizeof(T) == 4)
+        if (vecs <= kWide / 2 * 512) return run_bwd_rows<T, V, kWide / 2, FORM, CK>(a, group(kWide / 2), dweight, dbias, ls);
+    if (vecs <= kWide * 512) return run_bwd_rows<T, V, kWide, FORM, CK>(a, group(kWide), dweight, dbias, ls);
     const int blocks = fewer(a.rows, 2 * kSms);
     launch(norm_bwd_long_rows_kernel<T, CK>, dim3(blocks), dim3(1024), 0, ls, a);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
 template <class T, bool CK> int bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
-    auto on_grid = [&](const void* p, long long stride, int v) { return !p || (aligned(p, v * sizeof(T)) && (a.rows == 1 || stride % v == 0)); };
-    auto fits = [&](int v) { return on_grid(a.x, a.x_stride, v) && on_grid(a.dy, a.dy_stride, v) && on_grid(a.out, a.out_stride, v); };
     constexpr int V = 16 / sizeof(T);
-    if (fits(V))
-        return a.c % V == 0 && a.weight && a.w_vec ? pick_bwd_rows<T, V, true, CK>(a, dweight, dbias, ls) : pick_bwd_rows<T, V, false, CK>(a, dweight, dbias, ls);
-    if constexpr (V == 8)
-        if (fits(2)) return pick_bwd_rows<T, 2, false, CK>(a, dweight, dbias, ls);
-    return pick_bwd_rows<T, 1, false, CK>(a, dweight, dbias, ls);
+    const bool one = a.rows == 1;
+    auto on_grid = [&](const void* p, long long stride) { return !p || (aligned(p, 16) && (one || stride % V == 0)); };
+    // the same distance above the grid as dy, in every row
+    auto like_dy = [&](const void* p, long long stride) {
+        return !p || (((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(a.dy)) & 15) == 0 && (one || (stride - a.dy_stride) % V == 0));
+    };
+    if (on_grid(a.x, a.x_stride) && on_grid(a.dy, a.dy_stride) && on_grid(a.out, a.out_stride))
+        return a.c % V == 0 && a.weight && a.w_vec ? pick_bwd_rows<T, V, kFast, CK>(a, dweight, dbias, ls) : pick_bwd_rows<T, V, kEdge, CK>(a, dweight, dbias, ls);
+    if (like_dy(a.x, a.x_stride) && like_dy(a.out, a.out_stride)) return pick_bwd_rows<T, V, kShift, CK>(a, dweight, dbias, ls);
+    return pick_bwd_rows<T, 1, kEdge, CK>(a, dweight, dbias, ls);
 }
 
 // Shape of a launch over maps: warps that share a tile's channels, channels of each, warps of a block.

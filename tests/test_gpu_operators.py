@@ -16,7 +16,7 @@ EPS = 1e-5
 SHAPES = [
     ((1, 1), 0, 0), ((3, 2), 0, 0), ((5, 7), 0, 0), ((33, 32), 0, 0), ((9, 33), 3, 1), ((1, 1024), 0, 0), ((17, 1000), 24, 0),
     ((6, 1111), 2, 3), ((300, 64), 0, 0), ((4, 4096), 0, 0), ((3, 5001), 0, 0), ((2, 9000), 0, 0), ((2, 20000), 0, 5), ((1, 40000), 8, 0),
-    ((1, 70001), 0, 0), ((700, 257), 1, 0),
+    ((1, 70001), 0, 0), ((700, 257), 1, 0), ((333, 372), 0, 0), ((1300, 1111), 2, 0), ((19, 4097), 0, 1), ((2500, 68), 3, 2), ((9, 2047), 6, 7),
     ((2, 3, 1, 2), 0, 0), ((1, 8, 13, 13), 0, 0), ((3, 32, 13, 13), 0, 0), ((2, 64, 16, 24), 0, 0), ((2, 21, 10, 6), 4, 2), ((1, 512, 7, 7), 0, 0),
     ((2, 100, 8, 8), 8, 8), ((1, 1030, 5, 4), 0, 0), ((1, 2100, 3, 11), 5, 1), ((40, 5, 1, 3), 0, 0), ((2, 4, 64, 70), 0, 0),
 ]
@@ -204,19 +204,28 @@ def test_ckpt_is_defined_to_the_bit(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("run", [(4, 96), (3, 45), (2, 3, 7, 9)])
-def test_ckpt_special_values(run, dtype):
+@pytest.mark.parametrize("shift", [0, 1, 3])
+@pytest.mark.parametrize("run", [(4, 96), (3, 45), (2, 2500), (3, 5003), (1, 9001), (2, 3, 7, 9)])
+def test_ckpt_special_values(run, shift, dtype):
+    """Blocks with infinities, NaNs and the largest values, from the call and from the norm's forward pass in place."""
     x = _normal(run, 22).to(dtype)
     f = x.reshape(-1)
     top = torch.finfo(dtype).max
     f[0], f[5], f[11] = float("inf"), float("nan"), -float("inf")
     f[33], f[34] = top, -top
     f[35] = torch.finfo(dtype).tiny
-    xd = x.cuda()
+    f[-1], f[f.numel() // 2] = float("nan"), float("inf")
+    xd, xg = guarded(x, 0, shift)
     ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
     ftp.ftp_ckpt_save(xd, ckpt)
-    back = torch.empty_like(xd)
+    there, tg = guarded(x, 0, shift)
+    beside = torch.empty_like(ckpt)
+    ftp.ftp_norm_forward(there, None, None, there, ckpt=beside)
+    assert torch.equal(ckpt, beside)
+    tg()
+    back, bg = guarded(torch.zeros_like(x), 0, shift)
     ftp.ftp_ckpt_load(ckpt, back)
+    xg(), bg()
     want = torch.from_numpy(eight_bits(x, _run(run))[0]).to(dtype)
     assert _same(back, want)
     assert torch.isfinite(back.cpu()[torch.isfinite(x)]).all()
@@ -431,6 +440,23 @@ def test_loss_gradient_against_differences(shape):
         up[i] += h
         down[i] -= h
         assert abs((f(up) - f(down)) / (2 * h) - float(dz.reshape(-1)[i])) <= 1e-6
+
+
+def test_backward_ckpt_is_load_forward_backward():
+    from paper_2409_09083_b200 import synth
+    for precision in (0, 1):
+        plan = ftp.ftp_plan([synth.conv(16, 8, 3), synth.pool()], 2, 16, 20, 28, (2, 2), ((1, 2),), precision=precision)
+        x, params, ws = _normal(plan.shape, 50).cuda(), 0.3 * _normal((plan.param_floats,), 51).cuda(), plan.new_workspace()
+        dy = _normal((plan.out_floats,), 52).cuda()
+        ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
+        ftp.ftp_ckpt_save(x, ckpt)
+        got, want = ([torch.empty_like(x), torch.empty_like(x), torch.empty_like(params)] for _ in range(2))
+        ftp.ftp_backward_ckpt(plan, ckpt, got[0], dy, params, got[1], got[2], ws)
+        ftp.ftp_ckpt_load(ckpt, want[0])
+        ftp.ftp_forward(plan, want[0], params, None, ws)
+        ftp.ftp_backward(plan, want[0], dy, params, want[1], want[2], ws)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
 
 
 # ---- streams, graphs, order -----------------------------------------------------------------------------------------
