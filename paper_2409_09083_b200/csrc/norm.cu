@@ -33,15 +33,15 @@ struct NormArgs {
     int w_vec;                   // weight and bias are 16-byte aligned
 };
 
-// Adds over the `tpr` threads of a group; tpr a power of two, groups within a warp, or the block (number 0), or a whole number of warps with a
-// barrier `number` of their own (an SM has 64 barriers and a kernel that names them at run time takes 16 a block: for kernels of one
+// Adds over the `tpr` threads of a group: a power of two of lanes, or whole warps -- the block, or with a barrier `number` of their own (an SM
+// has 64 barriers and a kernel that names them at run time takes 16 a block: for kernels of one
 // block an SM).  `red`: K floats a warp, not read or written by anyone else until the group has passed another barrier.
 template <int K, bool NAMED = false> __device__ __forceinline__ void group_sum(float (&v)[K], int tpr, int number, float* red)
 {
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = lanes_sum(v[k], tpr);
     if (tpr <= 32) return;
-    const int warp = threadIdx.x >> 5, per = tpr >> 5, first = warp & ~(per - 1);
+    const int warp = threadIdx.x >> 5, per = tpr >> 5, first = NAMED ? (number - 1) * per : 0;
     if ((threadIdx.x & 31) == 0) {
 #pragma unroll
         for (int k = 0; k < K; ++k) red[warp * K + k] = v[k];
@@ -355,12 +355,12 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
 {
     constexpr bool kWhole = FORM == kFast || V == 1;
     constexpr int E = V * VPT;
-    extern __shared__ float smem[];                    // a set of columns per group, to add the groups of the block
+    extern __shared__ __align__(16) float smem[];      // the weights of each thread's columns; at the end a set of columns per group, to be added
     __shared__ float red[2][32];
     __shared__ int shifts[64];
     previous_launches();
     next_launch();
-    const int per = blockDim.x / tpr, t = threadIdx.x & (tpr - 1), group = threadIdx.x / tpr;
+    const int per = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
     const float inv_c = 1.f / (float)a.c;
     Vals<E> dw = all<E>(0.f), db = all<E>(0.f);
     const long long step = (long long)gridDim.x * per;
@@ -378,6 +378,19 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
     at.rstd = a.rstd + row;
     RowIn<T, V, VPT, FORM == kShift, CK> next;
     load_row<T, V, VPT, FORM, CK>(a, at, row < a.rows, o, tpr, t, next);
+    float4* weights = reinterpret_cast<float4*>(smem) + threadIdx.x;
+    {
+        Vals<E> w = all<E>(0.f);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int e = (i * tpr + t) * V;
+            if (e < hi) load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v + i * V);
+        }
+        if constexpr (E % 4 == 0) {
+#pragma unroll
+            for (int j = 0; j < E; j += 4) weights[j / 4 * blockDim.x] = make_float4(w.v[j], w.v[j + 1], w.v[j + 2], w.v[j + 3]);
+        } else smem[threadIdx.x] = w.v[0];
+    }
     int turn = 0;
     // (groups narrower than a warp stay together: a warp goes on until none of its rows is left)
     for (long long first = (long long)blockIdx.x * per + (tpr < 32 ? (threadIdx.x & ~31) / tpr : group); first < a.rows; first += step, turn ^= 1) {
@@ -404,12 +417,14 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
         load_row<T, V, VPT, FORM, CK>(a, at, row < a.rows, o, tpr, t, next);
         dw = fma(d, hat, dw);
         db = add(db, d);
-        Vals<E> w = all<E>(0.f);                       // (from L1: 16 registers more would spill)
+        Vals<E> w;                                     // (16 registers more would spill)
+        if constexpr (E % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int e = (i * tpr + t) * V;
-            if (e < hi) load_cols<FORM == kFast, V>(a.weight, e - o, a.c, 1.f, w.v + i * V);
-        }
+            for (int j = 0; j < E; j += 4) {
+                const float4 q = weights[j / 4 * blockDim.x];
+                w.v[j] = q.x; w.v[j + 1] = q.y; w.v[j + 2] = q.z; w.v[j + 3] = q.w;
+            }
+        } else w.v[0] = smem[threadIdx.x];
         const Vals<E> g = mul(d, w);
         float s[2] = {sum_of(g), sum_of(mul(g, hat))};
         group_sum<2, true>(s, tpr, group + 1, red[turn]);
@@ -951,13 +966,14 @@ int sum_sets(const NormArgs& a, int sets, float* dweight, float* dbias, LaunchSt
 
 template <class T, int V, int VPT, int FORM, bool CK> int run_bwd_rows(const NormArgs& a, int tpr, float* dweight, float* dbias, LaunchStream ls)
 {
-    const int per = 512 / tpr;
-    const size_t smem = a.partials ? (size_t)512 * VPT * V * 4 : 0;
+    const int per = 512 / tpr, threads = per * tpr;
+    const size_t smem = (size_t)threads * VPT * V * 4;
     int blocks = fewer((a.rows + per - 1) / per, kSms);
     // rows of a group a multiple of V rows apart (unless each has one row only)
-    if (FORM == kShift && (long long)blocks * per < a.rows && per < V) blocks -= blocks % (V / per);
+    if (FORM == kShift && (long long)blocks * per < a.rows)
+        while ((blocks * per) % V) --blocks;
     if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, smem)) return FTP_ERR_CUDA;
-    launch(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, dim3(blocks), dim3(512), smem, ls, a, tpr);
+    launch(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, dim3(blocks), dim3(threads), smem, ls, a, tpr);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
 // 16 values to a thread (8 in fp32, whose values as read take the registers of two); rows of up to 8192 columns.
@@ -965,7 +981,10 @@ template <class T, int V, int FORM, bool CK> int pick_bwd_rows(const NormArgs& a
 {
     const long long vecs = (a.c + (FORM == kShift ? V - 1 : 0) + V - 1) / V;
     const int least = kBlock / V < 8 ? 8 : kBlock / V;
-    auto group = [&](int vpt) { const int t = pow2_at_least((vecs + vpt - 1) / vpt); return t < least ? least : t; };
+    auto group = [&](int vpt) {                            // lanes of a warp by powers of two, then whole warps
+        const long long t = (vecs + vpt - 1) / vpt;
+        return t > 32 ? (int)(t + 31) / 32 * 32 : pow2_at_least(t) < least ? least : pow2_at_least(t);
+    };
     constexpr int kWide = 16 / V;
     if (vecs <= 32) return run_bwd_rows<T, V, 1, FORM, CK>(a, group(1), dweight, dbias, ls);
     if constexpr (sizeof(T) == 4)
