@@ -598,11 +598,11 @@ __device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, 
     const long long run = t.n * a.c + t.first;
     char* qt = reinterpret_cast<char*>(a.ck.q + run * a.ck.pitch + t.px);
     unsigned char* et = a.ck.steps + run * a.ck.blocks + t.px / kBlock;
-    bool any = false;
+    if constexpr (CK) {                                         // the checkpoint first, before y may have been written over x
+        bool any = false;
 #pragma unroll
-    for (int i = 0; i < CPT; ++i) {
-        if (i >= count) continue;
-        if (CK) {                                               // as if all values were finite
+        for (int i = 0; i < CPT; ++i) {                         // as if all values were finite
+            if (i >= count) continue;
             const Vals<V> v = values(raw[i]);
             const float big = largest(v);
             any |= special<T>(big);
@@ -612,25 +612,30 @@ __device__ __forceinline__ void norm_fwd_tile(const NormArgs& a, const Tile& t, 
                 if (t.px % kBlock == 0) et[(unsigned long long)(unsigned)a.ck.blocks * i] = (unsigned char)ex;
             }
         }
-        if (live) {
-            const float2 c = wb[t.first + i];
-            store_pack<T, V>(reinterpret_cast<T*>(plane(yt, bytes, i)),
-                             rounded<T, V>(fma(add(values(raw[i]), minus), mul(rstd, all<V>(c.x)), all<V>(c.y))));
-        }
-    }
-    if (CK && __any_sync(0xffffffffu, any)) {                   // the blocks with others once more
-#pragma unroll
-        for (int i = 0; i < CPT; ++i) {
-            if (i >= count) continue;
-            const Vals<V> v = values(raw[i]);
-            if (!special<T>(largest(v))) continue;
-            unsigned ex;
-            const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
-            if (FULL || t.px < a.ck.pitch) {
-                store_pack<unsigned char, V>(reinterpret_cast<unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)), st);
-                if (t.px % kBlock == 0) et[(unsigned long long)(unsigned)a.ck.blocks * i] = (unsigned char)ex;
+        if (__any_sync(0xffffffffu, any)) {                     // the blocks with others once more
+#pragma unroll 1
+            for (int i = 0; i < count; ++i) {
+                Pack<T, V> again = zero_pack<T, V>();
+                if (live) again = load_pack<T, V>(reinterpret_cast<const T*>(plane(xt, bytes, i)));
+                const Vals<V> v = values(again);
+                if (special<T>(largest(v))) {
+                    unsigned ex;
+                    const Pack<unsigned char, V> st = to_steps_special<T, V>(v, ex);
+                    if (FULL || t.px < a.ck.pitch) {
+                        store_pack<unsigned char, V>(reinterpret_cast<unsigned char*>(plane(qt, (unsigned)a.ck.pitch, i)), st);
+                        if (t.px % kBlock == 0) et[(unsigned long long)(unsigned)a.ck.blocks * i] = (unsigned char)ex;
+                    }
+                }
+                __syncwarp();
             }
         }
+    }
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+        if (i >= count || !live) continue;
+        const float2 c = wb[t.first + i];
+        store_pack<T, V>(reinterpret_cast<T*>(plane(yt, bytes, i)),
+                         rounded<T, V>(fma(add(values(raw[i]), minus), mul(rstd, all<V>(c.x)), all<V>(c.y))));
     }
 }
 
@@ -777,14 +782,15 @@ __device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, 
         shift.v[j] = live ? -a.mean[t.row + j] * rstd.v[j] : 0.f;
     }
     float sums[kOwn ? 1 : CPT];
-    Vals<V> hat[CPT];
+    constexpr bool kAgain = CK && V == 4;                       // steps are decoded twice: 32 registers of hats less
+    Vals<V> hat[kAgain ? 1 : CPT];
 #pragma unroll
     for (int i = 0; i < CPT; ++i) {
         if (!kOwn) sums[i] = 0.f;
         if (i >= count) continue;
         const float w = wb[t.first + i].x;
-        hat[i] = x[i].hats(rstd, shift);
-        const Vals<V> d = values(dy[i]), dh = mul(d, hat[i]);
+        hat[kAgain ? 0 : i] = x[i].hats(rstd, shift);
+        const Vals<V> d = values(dy[i]), dh = mul(d, hat[kAgain ? 0 : i]);
         s[0] = fma(d, all<V>(w), s[0]);
         s[1] = fma(dh, all<V>(w), s[1]);
         if constexpr (kOwn) { cs.dw[i] += sum_of(dh); cs.db[i] += sum_of(d); }
@@ -801,11 +807,15 @@ __device__ __forceinline__ void norm_bwd_tile(const NormArgs& a, const Tile& t, 
     if (!a.out) return;
     const Vals<V> m0 = mul(mul(s[0], all<V>(-inv_c)), rstd), m1 = mul(mul(s[1], all<V>(-inv_c)), rstd);
     char* out = reinterpret_cast<char*>(static_cast<T*>(a.out) + t.n * a.out_stride + at);
+    if constexpr (kAgain) {
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) asm volatile("" : "+r"(x[i].q.w[0]));       // (or the compiler keeps them after all)
+    }
 #pragma unroll
     for (int i = 0; i < CPT; ++i)
         if (i < count && live)
             store_pack<T, V>(reinterpret_cast<T*>(plane(out, bytes, i)),
-                             rounded<T, V>(fma(hat[i], m1, fma(values(dy[i]), mul(rstd, all<V>(wb[t.first + i].x)), m0))));
+                             rounded<T, V>(fma(kAgain ? x[i].hats(rstd, shift) : hat[kAgain ? 0 : i], m1, fma(values(dy[i]), mul(rstd, all<V>(wb[t.first + i].x)), m0))));
 }
 
 template <class T, int V, int CPT, bool CK>
@@ -1023,11 +1033,12 @@ MapShapeOf map_shape(int c, int most)
 template <class T, int V, bool CK> int fwd_map(const NormArgs& a, LaunchStream ls)
 {
     const long long tiles = (a.p + 32 * V - 1) / (32 * V), all = a.n * tiles;
-    if (a.c > 1024) {
-        launch(norm_fwd_long_map_kernel<T, V, CK>, dim3(fewer(all, 4 * kSms)), dim3(512), 0, ls, a, (int)tiles);
-        return launched();
-    }
-    const MapShapeOf m = map_shape(a.c, a.c <= 128 && (CK || V == 2) ? 16 : 32);
+    if constexpr (V < 4)
+        if (a.c > 1024) {
+            launch(norm_fwd_long_map_kernel<T, V, CK>, dim3(fewer(all, 4 * kSms)), dim3(512), 0, ls, a, (int)tiles);
+            return launched();
+        }
+    const MapShapeOf m = map_shape(a.c, V == 4 ? 8 : a.c <= 128 && (CK || V == 2) ? 16 : 32);
     const size_t smem = (size_t)a.c * 8 + 2 * (size_t)m.warps * 32 * V * 4;
     const long long blocks = (all + m.warps / m.share - 1) / (m.warps / m.share);
 #define GO(...)                                                                                                                             \
@@ -1040,21 +1051,25 @@ template <class T, int V, bool CK> int fwd_map(const NormArgs& a, LaunchStream l
     // a checkpoint to write the kernel is closer to the issue rate and takes all it can get (123 us with 16 warps, 111 with 24).
     const int cap = CK ? 32 : 16 / m.warps > 0 ? 16 / m.warps : 1;
     if (m.per <= 8 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 8, CK, 256>);
-    if constexpr (CK || V == 2)
-        if (m.per <= 16 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 16, CK, 256>);
-    if (m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 32, CK, 256>);
-    GO(norm_fwd_map_kernel<T, V, 32, CK, 1024>);
+    if constexpr (V == 4) GO(norm_fwd_map_kernel<T, V, 8, CK, 512>);
+    else {
+        if constexpr (CK || V == 2)
+            if (m.per <= 16 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 16, CK, 256>);
+        if (m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 32, CK, 256>);
+        GO(norm_fwd_map_kernel<T, V, 32, CK, 1024>);
+    }
 #undef GO
 }
 template <class T, int V, bool CK> int bwd_map(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
     const long long tiles = (a.p + 32 * V - 1) / (32 * V), all = a.n * tiles;
-    if (a.c > 512) {
-        const int blocks = fewer(all, 2 * kSms);
-        launch(norm_bwd_long_map_kernel<T, V, CK>, dim3(blocks), dim3(512 / V), 0, ls, a, (int)tiles);
-        return sum_sets(a, blocks, dweight, dbias, ls);
-    }
-    const MapShapeOf m = map_shape(a.c, CK && V == 2 && a.c <= 128 ? 8 : a.c <= 256 ? 16 : 32);
+    if constexpr (V < 4)
+        if (a.c > 512) {
+            const int blocks = fewer(all, 2 * kSms);
+            launch(norm_bwd_long_map_kernel<T, V, CK>, dim3(blocks), dim3(512 / V), 0, ls, a, (int)tiles);
+            return sum_sets(a, blocks, dweight, dbias, ls);
+        }
+    const MapShapeOf m = map_shape(a.c, V == 4 ? 8 : CK && V == 2 && a.c <= 128 ? 8 : a.c <= 256 ? 16 : 32);
     const size_t smem = (size_t)a.c * 8 + 4 * (size_t)m.warps * 32 * V * 4;
     const long long want = (all + m.warps / m.share - 1) / (m.warps / m.share);
 #define GO(...)                                                                                                    \
@@ -1064,30 +1079,40 @@ template <class T, int V, bool CK> int bwd_map(const NormArgs& a, float* dweight
         return sum_sets(a, blocks, dweight, dbias, ls);                                                            \
     } while (0)
     if (m.per <= 8) GO(norm_bwd_map_kernel<T, V, 8, CK>);
-    if (m.per <= 16) GO(norm_bwd_map_kernel<T, V, 16, CK>);
-    GO(norm_bwd_map_kernel<T, V, 32, CK>);
+    if constexpr (V < 4) {
+        if (m.per <= 16) GO(norm_bwd_map_kernel<T, V, 16, CK>);
+        GO(norm_bwd_map_kernel<T, V, 32, CK>);
+    } else return FTP_ERR_ARG;                            // (per is at most 8)
 #undef GO
 }
 
-// Whether arrays can be read as pairs of 16-bit pixels.
-template <class T> bool map_pairs(const NormArgs& a)
+// Whether arrays can be read v pixels at a time.
+template <class T> bool map_words(const NormArgs& a, int v)
 {
-    auto fits = [&](const void* p, long long stride) { return !p || (aligned(p, 4) && (a.n == 1 || stride % 2 == 0)); };
-    return a.p % 2 == 0 && fits(a.x, a.x_stride) && fits(a.dy, a.dy_stride) && fits(a.out, a.out_stride);
+    auto fits = [&](const void* p, long long stride) { return !p || (aligned(p, v * sizeof(T)) && (a.n == 1 || stride % v == 0)); };
+    return a.p % v == 0 && fits(a.x, a.x_stride) && fits(a.dy, a.dy_stride) && fits(a.out, a.out_stride);
 }
+// With a checkpoint, four pixels a lane and 8 channels a thread where 16 warps hold the channels that way: its addresses, exponents and bytes
+// cost more than the arithmetic and are shared by four values then (8 x 64 x 208 x 208: one pixel and 16 channels 50 us forward, 54 us
+// backward).  Without one, more channels a thread and fewer barriers are worth more.
+template <class T, bool CK> bool map_quads(const NormArgs& a) { return CK && a.c <= 128 && map_words<T>(a, 4); }
 
 template <class T, bool CK> int forward(const NormArgs& a, LaunchStream ls)
 {
     if (a.p == 1) return fwd_rows<T, CK>(a, ls);
+    if constexpr (CK)
+        if (map_quads<T, CK>(a)) return fwd_map<T, 4, CK>(a, ls);
     if constexpr (sizeof(T) == 2)
-        if (map_pairs<T>(a)) return fwd_map<T, 2, CK>(a, ls);
+        if (map_words<T>(a, 2)) return fwd_map<T, 2, CK>(a, ls);
     return fwd_map<T, 1, CK>(a, ls);
 }
 template <class T, bool CK> int backward(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
     if (a.p == 1) return bwd_rows<T, CK>(a, dweight, dbias, ls);
+    if constexpr (CK)
+        if (map_quads<T, CK>(a)) return bwd_map<T, 4, CK>(a, dweight, dbias, ls);
     if constexpr (sizeof(T) == 2)
-        if (map_pairs<T>(a)) return bwd_map<T, 2, CK>(a, dweight, dbias, ls);
+        if (map_words<T>(a, 2)) return bwd_map<T, 2, CK>(a, dweight, dbias, ls);
     return bwd_map<T, 1, CK>(a, dweight, dbias, ls);
 }
 template <class T> int forward(const NormArgs& a, bool ck, LaunchStream ls) { return ck ? forward<T, true>(a, ls) : forward<T, false>(a, ls); }
