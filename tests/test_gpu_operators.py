@@ -514,6 +514,87 @@ def test_graph_side_stream_and_repeat_give_the_same_bits(shape):
         assert torch.equal(first[k], held[k]), k
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(6, 372), (40, 1111), (3, 5001), (2, 9001), (2, 40, 10, 6)])
+def test_arrays_of_different_alignment(shape, dtype):
+    """Every array another distance off the 16-byte grid, and another stride between samples: the same results as dense ones."""
+    x, dy, w = _normal(shape, 60, dtype), _normal(shape, 61, dtype), _normal(shape[1:2], 62).cuda()
+    labels = torch.randint(-1, shape[1], _rows_of(shape), generator=torch.Generator().manual_seed(3)).cuda()
+    dense = _buffers(x.cuda(), labels)
+    ftp.ftp_norm_forward(x.cuda(), w, w, dense["y"], dense["mean"], dense["rstd"])
+    ftp.ftp_norm_backward(x.cuda(), dy.cuda(), w, dense["mean"], dense["rstd"], dense["dx"], dense["dw"], dense["db"], dense["nws"])
+    ftp.ftp_logprob(x.cuda(), labels, dense["logp"], dense["lse"], dense["entropy"])
+    ftp.ftp_loss_logprob(x.cuda(), labels, dense["dz"], dense["loss"], dense["lws"], scale=100.0)
+    ftp.ftp_logprob_backward(x.cuda(), labels, dense["lse"], dense["entropy"], dense["mean"], dense["rstd"], dense["dz2"])
+    xd, xg = guarded(x, 3, 1)
+    dyd, dyg = guarded(dy, 6, 2)
+    outs = [guarded(torch.zeros_like(x), pad, shift) for pad, shift in ((0, 3), (5, 0), (1, 5), (2, 6))]
+    (y, yg), (dx, dxg), (dz, dzg), (dz2, dz2g) = outs
+    got = _buffers(x.cuda(), labels)
+    u = HALF_STEP[dtype]
+    ftp.ftp_norm_forward(xd, w, w, y, got["mean"], got["rstd"])
+    ftp.ftp_norm_backward(xd, dyd, w, dense["mean"], dense["rstd"], dx, got["dw"], got["db"], got["nws"])
+    ftp.ftp_loss_logprob(xd, labels, dz, got["loss"], got["lws"], scale=100.0)
+    ftp.ftp_logprob_backward(xd, labels, dense["lse"], dense["entropy"], dense["mean"], dense["rstd"], dz2)
+    # other kernels, other orders of the same sums: both are within 64 half-units of the terms' magnitude and half a step of the type
+    for a, b, size in ((y, dense["y"], 8.0), (dx, dense["dx"], 30.0), (dz, dense["dz"], 100.0 / max(1, int((labels >= 0).sum()))), (dz2, dense["dz2"], 30.0)):
+        a, b = a.cpu().double(), b.cpu().double()
+        assert ((a - b).abs() <= 2 * (u * b.abs() + TINY[dtype] + 64 * U * size)).all()
+    terms = float((dy.double().abs()).sum())
+    assert (got["dw"] - dense["dw"]).abs().max() <= 2e-5 * terms and (got["db"] - dense["db"]).abs().max() <= 2e-5 * terms
+    assert abs(got["loss"].item() - dense["loss"].item()) <= 1e-5 * (1 + abs(dense["loss"].item()))
+    for check in (xg, dyg, yg, dxg, dzg, dz2g):
+        check()
+
+
+def test_offsets_past_32_bits():
+    """Five samples 2^29 + 8 values apart: the last one starts past 2^31 values and 2^32 bytes."""
+    stride, n = (1 << 29) + 8, 5
+    whole = torch.empty((n - 1) * stride + 4096, dtype=torch.float16, device="cuda")
+    for shape in ((n, 1003), (n, 12, 10, 9)):
+        per = int(np.prod(shape[1:]))
+        view = torch.as_strided(whole, (n, per), (stride, 1))
+        view = view if len(shape) == 2 else view.unflatten(1, shape[1:])
+        x = _normal(shape, 70).half()
+        view.copy_(x)
+        labels = torch.zeros(_rows_of(shape), dtype=torch.int64, device="cuda")
+        want, got = _buffers(x.cuda(), labels), _buffers(x.cuda(), labels)
+        for out, src in ((want, x.cuda()), (got, view)):
+            ftp.ftp_ckpt_save(src, out["ckpt"])
+            ftp.ftp_logprob(src, labels, out["logp"], out["lse"], out["entropy"], out["tl"], out["ti"])
+            ftp.ftp_norm_forward(src, None, None, src, out["mean"], out["rstd"])
+            out["y"].copy_(src)
+            ftp.ftp_norm_backward(None, src, None, out["mean"], out["rstd"], src, out["dw"], out["db"], out["nws"], ckpt=out["ckpt"])
+            out["dx"].copy_(src)
+            ftp.ftp_loss_logprob(src, labels, src, out["loss"], out["lws"])
+            out["dz"].copy_(src)
+            ftp.ftp_ckpt_load(out["ckpt"], src)
+            out["back"].copy_(src)
+        for k in ("ckpt", "logp", "lse", "entropy", "tl", "ti", "mean", "rstd", "y", "dx", "dw", "db", "loss", "dz", "back"):
+            close(got[k], want[k], 1e-2 * (1 + want[k].double().abs()) if k in ("y", "dx", "dz", "loss", "dw", "db") else 4e-6 * (1 + want[k].double().abs()), k)
+
+
+def test_two_streams_at_once():
+    """Calls that share nothing but their inputs, on two streams with workspaces of their own."""
+    shape = (700, 4000)
+    x, dy, w = _normal(shape, 80).cuda(), _normal(shape, 81).cuda(), _normal(shape[1:2], 82).cuda()
+    labels = torch.randint(0, shape[1], (shape[0],), generator=torch.Generator().manual_seed(5)).cuda()
+    pack = dy[:, :1].contiguous()
+    alone = _buffers(x, labels)
+    _everything(x, pack, w, labels, alone)
+    torch.cuda.synchronize()
+    both = [_buffers(x, labels) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for out, s in zip(both, streams):
+            with torch.cuda.stream(s):
+                _everything(x, pack, w, labels, out)
+    torch.cuda.synchronize()
+    for out in both:
+        for k in _RESULTS:
+            assert torch.equal(out[k], alone[k]), k
+
+
 def test_empty_arrays():
     w = torch.full((6,), GUARD, device="cuda")
     for shape in ((0, 6), (2, 6, 0, 3)):
