@@ -849,8 +849,10 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
     }
 }
 
-template <class T, int V, int CPT, int MODE, bool TOP>
-__global__ void __launch_bounds__(32 * kMapWarps) logprob_map_kernel(LpArgs a, int share, int per, int tiles)
+// MOST: warps of a block at most.  Blocks of four are held to 64 registers in the loss, for 32 warps an SM (90 registers and 20 warps: a map of
+// 21 classes and 416 x 416 pixels takes 59 us instead of 55).
+template <class T, int V, int CPT, int MODE, bool TOP, int MOST>
+__global__ void __launch_bounds__(32 * MOST, MOST == 4 && MODE == kLoss ? 8 : 1) logprob_map_kernel(LpArgs a, int share, int per, int tiles)
 {
     __shared__ float red[3][32 * kMapWarps * V];
     __shared__ unsigned long long keys[2][TOP ? 32 * kMapWarps : 1];
@@ -1114,10 +1116,13 @@ template <class T, int V, int MODE, bool TOP> int run_map(const LpArgs& a, int* 
         launch(__VA_ARGS__, dim3(*blocks), dim3(warps * 32), 0, ls, a, share, per, (int)tiles);                                              \
         return launched();                                                                                                                   \
     } while (0)
-    if (per <= 8) GO(logprob_map_kernel<T, V, 8, MODE, TOP>);
-    if (per <= 24) GO(logprob_map_kernel<T, V, 24, MODE, TOP>);
-    if (per <= 32) GO(logprob_map_kernel<T, V, 32, MODE, TOP>);
-    GO(logprob_map_kernel<T, V, 0, MODE, TOP>);
+    if (warps <= 4) {
+        if (per <= 8) GO(logprob_map_kernel<T, V, 8, MODE, TOP, 4>);
+        if (per <= 24) GO(logprob_map_kernel<T, V, 24, MODE, TOP, 4>);
+        GO(logprob_map_kernel<T, V, 32, MODE, TOP, 4>);
+    }
+    if (per <= 32) GO(logprob_map_kernel<T, V, 32, MODE, TOP, kMapWarps>);
+    GO(logprob_map_kernel<T, V, 0, MODE, TOP, kMapWarps>);
 #undef GO
 }
 
