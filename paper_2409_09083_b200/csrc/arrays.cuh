@@ -503,9 +503,10 @@ inline CkptView ckpt_view(const ftp_dims* d, const void* ckpt)
     return v;
 }
 
+// Dynamic shared memory of a launch; 48 KB together with the kernel's own (16 KB at most here) need no leave.
 template <class K> inline bool allow_smem(K kernel, size_t bytes)
 {
-    return bytes <= 48 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    return bytes <= 32 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
 }
 // Blocks of a kernel that an SM holds at once, from its registers (asked for once) and the launch's shared memory: persistent grids are
 // that many an SM, or their last blocks would wait for the first to end.
