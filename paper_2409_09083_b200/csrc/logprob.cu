@@ -11,6 +11,8 @@
 // A value and its class make one 64-bit key whose order is descending value, then ascending class.
 #include <cooperative_groups.h>
 
+#include <atomic>
+
 #include "arrays.cuh"
 
 using namespace ftp;
@@ -1041,7 +1043,28 @@ template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(co
     while (fit > 1 && 2 * fit * stage > kRingBytes) --fit;
     int stages = kRingBytes / (fit * stage);
     if (stages > 4) stages = 4;
-    const long long slots = (long long)kSms * fit / cluster, each = (a.rows + slots - 1) / slots;      // rows of a block: no more stages than that
+    const size_t ring = (size_t)stages * stage;
+    long long slots = (long long)kSms * fit;
+    if (cluster > 1) {
+        // a cluster stays within a GPC, whose SMs it need not divide: clusters that are not held at once would run after the others, each
+        // with as many rows (399 bf16 rows of 84120 classes and their gradient: 146 us with 148 / 4 clusters, 99 with those that fit)
+        static std::atomic<int> held[5][33];
+        std::atomic<int>& at = held[31 - __builtin_clz(cluster)][fit];
+        if (at.load(std::memory_order_relaxed) == 0) {
+            cudaLaunchAttribute dim{};
+            dim.id = cudaLaunchAttributeClusterDimension;
+            dim.val.clusterDim.x = cluster; dim.val.clusterDim.y = dim.val.clusterDim.z = 1;
+            cudaLaunchConfig_t ask{};
+            ask.gridDim = dim3(cluster); ask.blockDim = dim3(threads); ask.dynamicSmemBytes = ring; ask.attrs = &dim; ask.numAttrs = 1;
+            int n = 0;
+            if (!allow_smem(kernel, ring) ||
+                (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+                cudaOccupancyMaxActiveClusters(&n, kernel, &ask) != cudaSuccess || n < 1) return FTP_ERR_CUDA;
+            at.store(n, std::memory_order_relaxed);
+        }
+        slots = at.load(std::memory_order_relaxed);
+    }
+    const long long each = (a.rows + slots - 1) / slots;      // rows of a block: no more stages than that
     if (stages > each) stages = (int)each;
     const size_t smem = (size_t)stages * stage;
     *blocks = (int)(a.rows < slots ? a.rows : slots) * cluster;
@@ -1069,8 +1092,9 @@ template <class T, bool SHIFT, int MODE> int pick_block_rows(const LpArgs& a, bo
     while (cluster < 16 && a.rows * cluster * 2 <= kSms && share() > 512) cluster *= 2;
     constexpr bool kFin = MODE == kStats;
     if constexpr (MODE == kStats) {
-        // a warp a row from 12 rows an SM on: 50 KB of loads on their way there
-        if (a.rows >= 12 * kSms) {
+        // a warp a row from 12 rows an SM on: 50 KB of loads on their way there; and from 3 on where a row would take a cluster
+        // (fp16, us, warps against clusters: 900 rows of 50000 54 against 98, 552 of 56414 61 against 70, 414 of 117807 93 against 80)
+        if (a.rows >= (cluster > 1 ? 3 : 12) * kSms) {
             const int fit = resident<logprob_stream_rows_kernel<T, SHIFT>>(kStreamWarps * 32, 0);
             const long long want = (a.rows + kStreamWarps - 1) / kStreamWarps, most = (long long)kSms * fit;
             *blocks = (int)(want < most ? want : most);
