@@ -522,7 +522,8 @@ int ftp_backward_ckpt(ftp_plan* plan, const void* ckpt, float* x, const float* d
  *   mean = (1/c) sum x,  rstd = 1 / sqrt((1/c) sum (x - mean)^2 + eps),  y = (x - mean) rstd weight + bias.
  * weight, bias: device, c floats, each may be NULL (1 and 0).  mean, rstd: device, n p floats, each may be NULL; the backward pass needs
  * them.  eps >= 0 and finite.  y may be x.
- * ckpt (may be NULL) receives the checkpoint of x, as by ftp_ckpt_save, from the same reading of x.
+ * ckpt (may be NULL) receives the checkpoint of x, as by ftp_ckpt_save, from the same reading of x; with it the sums may be taken in
+ * another order than without, so that y, mean and rstd may differ in their last bits.
  */
 int ftp_norm_forward(const ftp_dims* d, const void* x, long long x_stride, const float* weight, const float* bias, float eps,
                      void* y, long long y_stride, float* mean, float* rstd, void* ckpt, void* stream);

@@ -14,15 +14,29 @@ taken at maps that are off by at most 1/127 of the largest magnitude among 32 ne
 
 Parameters are one flat vector: plan 0, weight and bias of the norm behind it, plan 1, ...
 """
+import functools
+
 import torch
 
 from . import binding as ftp
 from . import synth
 
 
+def _on_its_device(run):
+    """A chain's calls with its device current: the plans' calls take that one's current stream, as the operators between them do."""
+    @functools.wraps(run)
+    def call(self, *args, **kwargs):
+        if self.workspace.is_cuda:
+            with torch.cuda.device(self.workspace.device):
+                return run(self, *args, **kwargs)
+        return run(self, *args, **kwargs)
+    return call
+
+
 class Chain:
     def __init__(self, plans, eps=1e-5, device="cuda"):
-        """plans: ftp plans in order; the output map of each has the shape of the next one's input."""
+        """plans: ftp plans in order (one may come several times, with parameters of its own in each place); the output map of each
+        has the shape of the next one's input."""
         if not plans:
             raise ValueError("a chain needs at least one plan")
         self.plans, self.eps, self.device = list(plans), eps, torch.device(device)
@@ -34,8 +48,8 @@ class Chain:
             if tuple(p.shape) != self.shapes[i]:
                 raise ValueError(f"plan {i} gives a map {self.shapes[i]}, plan {i + 1} takes {tuple(p.shape)}")
         self.slices, at = [], 0                               # (plan, weight, bias) of each joint, (plan,) of the last
-        for p, s in zip(self.plans, self.shapes):
-            sizes = [p.param_floats] if p is self.plans[-1] else [p.param_floats, s[1], s[1]]
+        for i, (p, s) in enumerate(zip(self.plans, self.shapes)):
+            sizes = [p.param_floats] if i + 1 == len(self.plans) else [p.param_floats, s[1], s[1]]
             self.slices.append([slice(at + sum(sizes[:k]), at + sum(sizes[:k + 1])) for k in range(len(sizes))])
             at += sum(sizes)
         self.param_floats = at
@@ -65,6 +79,7 @@ class Chain:
         s = self.shapes[i]
         return self.maps[k][:_count(s)].view(s)
 
+    @_on_its_device
     def forward(self, x, params, y=None, keep=False, stream=None):
         """Logits of the last plan ([N, classes, H, W]), in `y` or a buffer of the chain; keep: the checkpoints for a backward pass."""
         self._check(x, params)
@@ -81,10 +96,12 @@ class Chain:
                 cur = out
         return out
 
+    @_on_its_device
     def answer(self, x, params, top_logp, top_index, entropy=None, stream=None):
         """The best classes of every pixel with their log probabilities ([N, k, H, W]), and the entropies."""
         ftp.ftp_logprob(self.forward(x, params, stream=stream), None, entropy=entropy, top_logp=top_logp, top_index=top_index, stream=stream)
 
+    @_on_its_device
     def step_grad(self, x, labels, params, dparams, loss_out, dx=None, stream=None):
         """Loss (mean over the labelled pixels of -log p) and gradient of one batch; labels: int64 [N, H, W] of the last map."""
         self._check(x, params)
@@ -112,6 +129,7 @@ class Chain:
                 ftp.ftp_forward(self.plans[0], x, params[sl[0]], None, ws, stream=stream)
                 ftp.ftp_backward(self.plans[0], x, d, params[sl[0]], dx, dparams[sl[0]], ws, stream=stream)
 
+    @_on_its_device
     def step(self, x, labels, params, dparams, lr, loss_out, dx=None, stream=None):
         """One training step: step_grad, then params -= lr dparams."""
         self.step_grad(x, labels, params, dparams, loss_out, dx=dx, stream=stream)
@@ -122,6 +140,9 @@ class Chain:
             raise ValueError(f"params has {params.numel()} elements, the chain needs {self.param_floats}")
         if x.numel() != self.plans[0].in_floats:
             raise ValueError(f"x has {x.numel()} elements, the chain needs {self.plans[0].in_floats}")
+        for t, name in ((x, "x"), (params, "params")):
+            if t.device != self.workspace.device:
+                raise ValueError(f"{name} is on {t.device}, the chain on {self.workspace.device}")
 
 
 def _count(shape):

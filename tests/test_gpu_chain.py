@@ -162,3 +162,62 @@ def test_one_plan_is_a_chain_too():
     ftp.ftp_loss_logprob(y, labels.cuda(), dy, loss2, chain.loss_ws)
     ftp.ftp_backward(plan, x.cuda(), dy, params.cuda(), dx2, again, ws)
     assert torch.equal(dparams, again) and torch.equal(dx, dx2) and torch.equal(loss, loss2)
+
+
+def test_inputs_of_another_device():
+    plans = _plans()
+    chain = chains.Chain(plans, device="cpu")
+    x, params = torch.zeros(plans[0].in_floats), torch.zeros(chain.param_floats)
+    with pytest.raises(ValueError, match="x is on meta, the chain on cpu"):
+        chain.forward(x.to("meta"), params)
+    with pytest.raises(ValueError, match="params is on meta"):
+        chain.answer(x, params.to("meta"), None, None)
+
+
+def _odd_plans(n=2, h=10, w=14, precision=0):
+    """13 channels at every joint, so that no part of the parameters after the first starts on 16 bytes."""
+    def make(layers, c):
+        return ftp.ftp_plan(layers, n, c, h, w, (2, 2), ((1, len(layers)),), precision=precision)
+    return make([synth.conv(3, 13, 3)], 3), lambda: make([synth.conv(13, 13, 3)], 13)
+
+
+def test_a_plan_in_two_places_has_parameters_in_each():
+    first, middle = _odd_plans()
+    again = middle()
+    chain = chains.Chain([first, again, again], device="cpu")
+    assert [len(sl) for sl in chain.slices] == [3, 3, 1]
+    assert chain.param_floats == first.param_floats + 2 * again.param_floats + 4 * 13
+    assert chain.slices[1][0].stop - chain.slices[1][0].start == chain.slices[2][0].stop - chain.slices[2][0].start == again.param_floats
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("precision", [0, 1])
+def test_parameters_off_the_16_byte_grid_and_a_plan_in_two_places(precision):
+    first, middle = _odd_plans(precision=precision)
+    again = middle()
+    chain, apart = chains.Chain([first, again, again]), chains.Chain([first, middle(), middle()])
+    x, params, labels = _batch(chain, 4)
+    x, params, labels = x.cuda(), params.cuda(), labels.cuda()
+    assert any(sl[0].start % 4 for sl in chain.slices)
+    grads, losses = [], []
+    for c in (chain, apart):
+        dparams, loss = torch.full((c.param_floats,), float("nan"), device="cuda"), torch.empty(1, device="cuda")
+        c.step_grad(x, labels, params, dparams, loss)
+        grads.append(dparams)
+        losses.append(loss)
+    assert torch.equal(grads[0], grads[1]) and torch.equal(losses[0], losses[1]) and torch.isfinite(grads[0]).all()
+    # the same calls, the norms' checkpoints among them (without, their sums have another order), with every part of the parameters in
+    # an array of its own
+    cur, ws = x, torch.empty(chain.workspace.numel(), dtype=torch.uint8, device="cuda")
+    for i, plan in enumerate(chain.plans):
+        part, out = [params[s].clone() for s in chain.slices[i]], torch.empty(chain.shapes[i], device="cuda")
+        ftp.ftp_forward(plan, cur, part[0], out, ws)
+        if i < 2:
+            ftp.ftp_norm_forward(out, part[1], part[2], out, eps=EPS, ckpt=torch.empty_like(chain.norm_ckpt[i]))
+            cur = out
+    assert torch.equal(out, chain.forward(x, params, keep=True))
+    delta, loss = torch.empty_like(out), torch.empty(1, device="cuda")
+    ftp.ftp_loss_logprob(out, labels, delta, loss, chain.loss_ws)
+    grad = torch.empty(again.param_floats, device="cuda")
+    ftp.ftp_backward(again, cur, delta, part[0], None, grad, ws)
+    assert torch.equal(grad, grads[0][chain.slices[2][0]]) and torch.equal(loss, losses[0])
