@@ -1,5 +1,9 @@
 """The channel norm, the 8-bit checkpoints, and the log probabilities of labels with their gradient and loss, against plain
 implementations in 64 bits, at the sizes, layouts and values where they can go wrong."""
+import pathlib
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -18,7 +22,7 @@ SHAPES = [
     ((6, 1111), 2, 3), ((300, 64), 0, 0), ((4, 4096), 0, 0), ((3, 5001), 0, 0), ((2, 9000), 0, 0), ((2, 20000), 0, 5), ((1, 40000), 8, 0),
     ((1, 70001), 0, 0), ((700, 257), 1, 0), ((333, 372), 0, 0), ((1300, 1111), 2, 0), ((19, 4097), 0, 1), ((2500, 68), 3, 2), ((9, 2047), 6, 7),
     ((2, 3, 1, 2), 0, 0), ((1, 8, 13, 13), 0, 0), ((3, 32, 13, 13), 0, 0), ((2, 64, 16, 24), 0, 0), ((2, 21, 10, 6), 4, 2), ((1, 512, 7, 7), 0, 0),
-    ((2, 100, 8, 8), 8, 8), ((1, 1030, 5, 4), 0, 0), ((1, 2100, 3, 11), 5, 1), ((40, 5, 1, 3), 0, 0), ((2, 4, 64, 70), 0, 0),
+    ((400, 9001), 1, 3), ((160, 16384), 0, 0), ((2, 100, 8, 8), 8, 8), ((1, 1030, 5, 4), 0, 0), ((1, 2100, 3, 11), 5, 1), ((40, 5, 1, 3), 0, 0), ((2, 4, 64, 70), 0, 0),
 ]
 
 
@@ -615,3 +619,38 @@ def test_empty_arrays():
         loss = torch.full((1,), GUARD, device="cuda")
         ftp.ftp_loss_logprob(x, labels, x, loss, torch.empty(ftp.ftp_loss_logprob_workspace_bytes(x), dtype=torch.uint8, device="cuda"))
         assert loss.item() == 0.0
+
+
+def test_the_first_calls_of_a_process_can_be_captured():
+    """Launch sizes that a process asks the runtime for once, attributes and lazily loaded kernels: none needs a call before the capture."""
+    code = """
+import torch
+import paper_2409_09083_b200 as ftp
+gen = torch.Generator().manual_seed(5)
+new = lambda *s, dtype=torch.float32: torch.empty(s, dtype=dtype, device="cuda")
+z = torch.randn((90, 40001), generator=gen).cuda()
+labels = torch.randint(0, 40001, (90,), generator=gen).cuda()
+x, dy = torch.randn((60, 700), generator=gen).cuda(), torch.randn((60, 700), generator=gen).cuda()
+ws, lws = (new(n, dtype=torch.uint8) for n in (ftp.ftp_norm_workspace_bytes(x), ftp.ftp_loss_logprob_workspace_bytes(z)))
+def run(o):
+    ftp.ftp_norm_forward(x, None, None, o[0], o[1], o[2], ckpt=o[3])
+    ftp.ftp_ckpt_load(o[3], o[4])
+    ftp.ftp_norm_backward(x, dy, None, o[1], o[2], o[5], o[6], o[7], ws)
+    ftp.ftp_logprob(z, labels, logp=o[8], lse=o[9], top_logp=o[10], top_index=o[11])
+    ftp.ftp_loss_logprob(z, labels, o[12], o[13], lws)
+def outs():
+    k = new(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8)
+    return [new(60, 700), new(60), new(60), k, new(60, 700), new(60, 700), new(700), new(700), new(90), new(90), new(90, 5),
+            new(90, 5, dtype=torch.int64), new(90, 40001), new(1)]
+held, eager = outs(), outs()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    run(held)
+g.replay()
+run(eager)
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(held, eager))
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=pathlib.Path(__file__).resolve().parents[1], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
