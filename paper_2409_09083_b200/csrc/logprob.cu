@@ -193,11 +193,10 @@ template <class F> __device__ __forceinline__ void place(const unsigned long lon
     }
 }
 
-// Sums of `n` warps, a power of two up to 32; every lane has them.
-__device__ __forceinline__ Sums join_lanes(const Sums* of, int n)
+// Sums of `n` lanes, a power of two up to 32, of which lane i has those numbered i modulo n; every lane has the result.
+__device__ __forceinline__ Sums join_lanes(Sums s, int n)
 {
     const int lane = threadIdx.x & 31;
-    Sums s = of[lane & (n - 1)];
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1)
         if (d < n) {
@@ -206,6 +205,8 @@ __device__ __forceinline__ Sums join_lanes(const Sums* of, int n)
         }
     return s;
 }
+
+__device__ __forceinline__ Sums join_lanes(const Sums* of, int n) { return join_lanes(of[threadIdx.x & (n - 1)], n); }
 
 // Adds a vector's exponents to the sums of a thread, which are A side by side.
 template <int MODE, int V, int A> __device__ __forceinline__ void take_sums(const Vals<V>& z, float shift, Vals<A>& s, Vals<A>& t)
@@ -483,12 +484,12 @@ constexpr int kRingBytes = 200 * 1024;
 
 struct BlockShared {
     unsigned long long list[kListBlock];
-    unsigned long long best[kTop];               // a block's own best, for the cluster
+    unsigned long long best[2][kTop];            // a block's own best, for the cluster; of this row and the one before
     unsigned long long round[32];
     float parts[kParts];
     Sums sums[2][32];                            // of the warps; of this row and the one before
     int count[2];
-    Sums whole;
+    Sums whole[2];
 };
 
 __device__ __forceinline__ void copy_16(void* to, const void* from)
@@ -644,17 +645,17 @@ logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_v
         if (!FIN && cluster > 1) {
             cg::cluster_group cl = cg::this_cluster();
             if (want_top) {
-                if (t < kTop) sh.best[t] = 0;
+                if (t < kTop) sh.best[turn][t] = 0;
                 __syncthreads();
-                place(sh.list, found, a.top, t, TH, [&](int at, unsigned long long k) { sh.best[at] = k; });
+                place(sh.list, found, a.top, t, TH, [&](int at, unsigned long long k) { sh.best[turn][at] = k; });
             }
-            if (t == 0) sh.whole = sums;
+            if (t == 0) sh.whole[turn] = sums;
+            // one barrier a row: what is read here is written again for the row after the next, behind the next row's barrier
             cl.sync();
-            sums = *cl.map_shared_rank(&sh.whole, 0);
-            for (int r = 1; r < cluster; ++r) sums = join(sums, *cl.map_shared_rank(&sh.whole, r));
+            if (MODE == kLoss || rank == 0) sums = join_lanes(*cl.map_shared_rank(&sh.whole[turn], lane & (cluster - 1)), cluster);
             if (want_top && rank == 0) {
                 found = cluster * a.top;
-                for (int i = t; i < found; i += TH) sh.list[i] = cl.map_shared_rank(sh.best, i / a.top)[i % a.top];
+                for (int i = t; i < found; i += TH) sh.list[i] = cl.map_shared_rank(sh.best[turn], i / a.top)[i % a.top];
                 __syncthreads();
             }
         }
@@ -687,8 +688,8 @@ logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_v
                 }
             }
         }
-        if (!FIN && cluster > 1) cg::this_cluster().sync();       // the others read this block's part
     }
+    if (!FIN && cluster > 1) cg::this_cluster().sync();           // the others read this block's part
     wait_rows(0);
     if (MODE == kLoss && a.sums && t == 0) a.sums[blockIdx.x] = total;
 }
