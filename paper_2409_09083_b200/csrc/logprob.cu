@@ -1093,9 +1093,10 @@ template <class T, bool SHIFT, int MODE> int pick_block_rows(const LpArgs& a, bo
     while (cluster < 16 && a.rows * cluster * 2 <= kSms && share() > 512) cluster *= 2;
     constexpr bool kFin = MODE == kStats;
     if constexpr (MODE == kStats) {
-        // a warp a row from 12 rows an SM on: 50 KB of loads on their way there; and from 3 on where a row would take a cluster
-        // (fp16, us, warps against clusters: 900 rows of 50000 54 against 98, 552 of 56414 61 against 70, 414 of 117807 93 against 80)
-        if (a.rows >= (cluster > 1 ? 3 : 12) * kSms) {
+        // a warp a row from 8 rows an SM on, and from 3 on where a row would take a cluster (us with 8 best classes, warps against
+        // blocks: bf16 1200 rows of 16000 21 against 30, f32 1200 of 5000 13 against 20, f16 1200 of 32000 42 against 40, bf16 1000 of
+        // 32000 37 against 33; against clusters: 900 of 50000 54 against 89, f32 600 of 120000 208 against 266, 300 of them 200 against 136)
+        if (a.rows >= (cluster > 1 ? 3 : 8) * kSms) {
             const int fit = resident<logprob_stream_rows_kernel<T, SHIFT>>(kStreamWarps * 32, 0);
             const long long want = (a.rows + kStreamWarps - 1) / kStreamWarps, most = (long long)kSms * fit;
             *blocks = (int)(want < most ? want : most);

@@ -250,7 +250,7 @@ CLASSES = [
     ((1, 1), 0, 0), ((4, 2), 0, 0), ((3, 5), 2, 1), ((65, 32), 0, 0), ((9, 33), 0, 0), ((1, 1000), 0, 0), ((40, 1000), 8, 0), ((7, 1025), 0, 3),
     ((5, 2049), 0, 0), ((3, 4097), 1, 1), ((2, 20011), 0, 0), ((1, 32000), 0, 0), ((310, 5000), 0, 0), ((1, 131072), 0, 0), ((2, 131071), 0, 0),
     ((1, 260000), 0, 1), ((1800, 2500), 0, 0), ((1777, 2311), 0, 1), ((24, 93590), 8, 0), ((30, 22001), 0, 0),
-    ((150, 10007), 1, 0), ((90, 40001), 1, 5), ((450, 33001), 0, 5),
+    ((150, 10007), 1, 0), ((1184, 2100), 0, 0), ((90, 40001), 1, 5), ((450, 33001), 0, 5),
     ((1, 2, 1, 3), 0, 0), ((2, 21, 8, 8), 0, 0), ((2, 80, 13, 13), 0, 0), ((1, 300, 9, 12), 8, 0), ((3, 70, 5, 5), 3, 1), ((1, 1500, 3, 4), 0, 0),
 ]
 
