@@ -503,10 +503,12 @@ inline CkptView ckpt_view(const ftp_dims* d, const void* ckpt)
     return v;
 }
 
-// Dynamic shared memory of a launch; 48 KB together with the kernel's own (16 KB at most here) need no leave.
-template <class K> inline bool allow_smem(K kernel, size_t bytes)
+// Dynamic shared memory of a launch; 48 KB together with the kernel's own (16 KB at most here) need no leave.  The leave is the process's, not
+// the launch's: `most`, what any launch of this kernel takes, is the only value that it is ever given, so that no thread lowers it between another
+// one's asking and its launch.
+template <class K> inline bool allow_smem(K kernel, size_t bytes, size_t most)
 {
-    return bytes <= 32 * 1024 || cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    return bytes <= 32 * 1024 || (bytes <= most && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) == cudaSuccess);
 }
 // Blocks of a kernel that an SM holds at once, from its registers (asked for once) and the launch's shared memory: persistent grids are
 // that many an SM, or their last blocks would wait for the first to end.

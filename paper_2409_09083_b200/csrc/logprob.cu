@@ -1060,7 +1060,7 @@ template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(co
             cudaLaunchConfig_t ask{};
             ask.gridDim = dim3(cluster); ask.blockDim = dim3(threads); ask.dynamicSmemBytes = ring; ask.attrs = &dim; ask.numAttrs = 1;
             int n = 0;
-            if (!allow_smem(kernel, ring) ||
+            if (!allow_smem(kernel, ring, kRingBytes) ||
                 (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
                 cudaOccupancyMaxActiveClusters(&n, kernel, &ask) != cudaSuccess || n < 1) return FTP_ERR_CUDA;
             at.store(n, std::memory_order_relaxed);
@@ -1079,7 +1079,7 @@ template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(co
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(*blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
-    if (!allow_smem(kernel, smem) ||
+    if (!allow_smem(kernel, smem, kRingBytes) ||
         (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) return FTP_ERR_CUDA;
     if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, share * (int)(16 / sizeof(T)), stages, dz_vec) != cudaSuccess) return FTP_ERR_CUDA;
     return launched();

@@ -982,7 +982,7 @@ template <class T, int V, int VPT, int FORM, bool CK> int run_bwd_rows(const Nor
     // rows of a group a multiple of V rows apart (unless each has one row only)
     if (FORM == kShift && (long long)blocks * per < a.rows)
         while ((blocks * per) % V) --blocks;
-    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, smem)) return FTP_ERR_CUDA;
+    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, smem, (size_t)512 * VPT * V * 4)) return FTP_ERR_CUDA;
     launch(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, dim3(blocks), dim3(threads), smem, ls, a, tpr);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }

@@ -3,6 +3,7 @@ implementations in 64 bits, at the sizes, layouts and values where they can go w
 import pathlib
 import subprocess
 import sys
+import threading
 
 import numpy as np
 import pytest
@@ -654,3 +655,67 @@ assert all(torch.equal(a, b) for a, b in zip(held, eager))
 """
     done = subprocess.run([sys.executable, "-c", code], cwd=pathlib.Path(__file__).resolve().parents[1], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+def _logprob_call(shape):
+    z = _normal(shape, 90).cuda()
+    labels = torch.randint(0, shape[1], shape[:1], generator=torch.Generator().manual_seed(6)).cuda()
+    logp, index = torch.zeros(shape[0], device="cuda"), torch.zeros((shape[0], 4), dtype=torch.int64, device="cuda")
+    return (logp, index), lambda: ftp.ftp_logprob(z, labels, logp, top_index=index)
+
+
+def _loss_call(shape):
+    z = _normal(shape, 91).cuda()
+    labels = torch.randint(0, shape[1], shape[:1], generator=torch.Generator().manual_seed(7)).cuda()
+    dz, loss = torch.zeros_like(z), torch.zeros(1, device="cuda")
+    ws = torch.empty(ftp.ftp_loss_logprob_workspace_bytes(z), dtype=torch.uint8, device="cuda")
+    return (dz, loss), lambda: ftp.ftp_loss_logprob(z, labels, dz, loss, ws)
+
+
+def _norm_backward_call(shape):
+    x, dy, w = _normal(shape, 92, torch.bfloat16).cuda(), _normal(shape, 93, torch.bfloat16).cuda(), _normal(shape[1:2], 94).cuda()
+    mean, rstd = torch.zeros(shape[0], device="cuda"), torch.ones(shape[0], device="cuda")
+    dx, dw, db = torch.zeros_like(x), torch.zeros_like(w), torch.zeros_like(w)
+    ws = torch.empty(ftp.ftp_norm_workspace_bytes(x), dtype=torch.uint8, device="cuda")
+    return (dx, dw, db), lambda: ftp.ftp_norm_backward(x, dy, w, mean, rstd, dx, dw, db, ws)
+
+
+@pytest.mark.parametrize("make, shapes", [(_logprob_call, ((600, 4100), (80, 9000))), (_loss_call, ((600, 4100), (80, 9000))),
+                                          (_norm_backward_call, ((40, 16384), (3, 8200)))], ids=["logprob", "loss", "norm backward"])
+def test_two_host_threads_call_one_kernel_with_much_and_little_shared_memory(make, shapes, monkeypatch):
+    """Calls of two threads share nothing but what both are given: what one asks of a kernel must not refuse the other one's launch.
+    The threads loop over the C entry itself; the binding's own work would leave them little time next to one another."""
+    want, threads, found, marshalled = [], [], [], []
+    for shape in shapes:
+        out, call = make(shape)
+        call()
+        want.append(out)
+    start = threading.Barrier(2, timeout=60)
+
+    def loop(entry, args, stream):
+        start.wait()
+        found.append([entry(*args, stream.cuda_stream) for _ in range(20000)])
+    results = []
+    for shape in shapes:
+        out, call = make(shape)
+        with monkeypatch.context() as m:
+            m.setattr(ftp.binding, "_call", lambda entry, x, name, stream, *args: marshalled.append((entry, args)))
+            call()
+        results.append((out, call))                           # (the call holds its inputs)
+        threads.append(threading.Thread(target=loop, args=marshalled[-1] + (torch.cuda.Stream(),)))
+    torch.cuda.synchronize()
+    interval = sys.getswitchinterval()
+    sys.setswitchinterval(1e-5)                               # (about the length of a call)
+    try:
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(interval)
+    torch.cuda.synchronize()
+    assert len(found) == 2
+    refused = [sum(rc != 0 for rc in codes) for codes in found]
+    assert refused == [0, 0], refused
+    for (out, _), first in zip(results, want):
+        assert all(torch.equal(a, b) for a, b in zip(out, first))
