@@ -14,6 +14,7 @@
 #include <atomic>
 
 #include "arrays.cuh"
+#include "row_ring.hpp"
 
 using namespace ftp;
 using namespace ftp::arr;
@@ -480,7 +481,6 @@ template <class T, bool SHIFT> __global__ void __launch_bounds__(kStreamWarps * 
 // What is left to do for a row once its sums and its list of candidates are there, a thousand cycles of one warp, is one more warp's
 // (FIN), while the others are at the next row.  Blocks of a cluster, and the loss, whose delta needs the sums at once, do without.
 constexpr int kStageMost = 64 * 1024;            // bytes of a part: 32768 classes of 16 bits, 16384 of 32
-constexpr int kRingBytes = 200 * 1024;
 
 struct BlockShared {
     unsigned long long list[kListBlock];
@@ -1025,13 +1025,13 @@ template <class T, int V> __global__ void __launch_bounds__(256) logprob_bwd_map
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------
-constexpr int kMostBlocks = 8 * kSms;         // blocks of a loss, each with a sum
+constexpr int kMostBlocks = kLossBlocksPerSm * kSms;         // blocks of a loss, each with a sum
 constexpr int kMostCounts = 1024;
 
 template <class T, int V, int NV, bool SHIFT, int MODE> int run_warp_rows(const LpArgs& a, int* blocks, cudaStream_t st)
 {
     const int fit = resident<logprob_warp_rows_kernel<T, V, NV, SHIFT, MODE>>(kRowWarps * 32, 0);
-    const long long want = (a.rows + kRowWarps - 1) / kRowWarps, most = (long long)kSms * (fit < 8 ? fit : 8);
+    const long long want = (a.rows + kRowWarps - 1) / kRowWarps, most = (long long)kSms * (fit < kLossBlocksPerSm ? fit : kLossBlocksPerSm);
     *blocks = (int)(want < most ? want : most);
     launch(logprob_warp_rows_kernel<T, V, NV, SHIFT, MODE>, dim3(*blocks), dim3(kRowWarps * 32), 0, LaunchStream{st, true}, a);
     return launched();
@@ -1040,11 +1040,9 @@ template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(co
 {
     auto kernel = logprob_block_rows_kernel<T, SHIFT, MODE, TH, FIN>;
     const int threads = TH + (FIN ? 32 : 0), stage = share * 16;
-    // rings of two stages at least, and of up to four where all the blocks that the registers allow still fit
-    int fit = resident<logprob_block_rows_kernel<T, SHIFT, MODE, TH, FIN>>(threads, 0);
-    while (fit > 1 && 2 * fit * stage > kRingBytes) --fit;
-    int stages = kRingBytes / (fit * stage);
-    if (stages > 4) stages = 4;
+    const RowRing shape = row_ring(resident<logprob_block_rows_kernel<T, SHIFT, MODE, TH, FIN>>(threads, 0), stage, MODE == kLoss);
+    const int fit = shape.blocks;
+    int stages = shape.stages;
     const size_t ring = (size_t)stages * stage;
     long long slots = (long long)kSms * fit;
     if (cluster > 1) {
@@ -1147,7 +1145,7 @@ template <class T, int V, int MODE, bool TOP> int run_map(const LpArgs& a, int* 
 #define GO(...)                                                                                                                              \
     do {                                                                                                                                     \
         const int fit = resident<__VA_ARGS__>(warps * 32, 0);                                                                                \
-        const long long want = (all + groups - 1) / groups, most = (long long)kSms * (fit < 8 ? fit : 8);                                    \
+        const long long want = (all + groups - 1) / groups, most = (long long)kSms * (fit < kLossBlocksPerSm ? fit : kLossBlocksPerSm);                                    \
         *blocks = (int)(want < most ? want : most);                                                                                          \
         launch(__VA_ARGS__, dim3(*blocks), dim3(warps * 32), 0, ls, a, share, per, (int)tiles);                                              \
         return launched();                                                                                                                   \
