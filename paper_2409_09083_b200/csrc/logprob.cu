@@ -342,6 +342,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) logprob_warp_rows_kernel(Lp
         }
         if (MODE == kLoss) {
             if (lane == 0 && label.has) total += logp_of_label(r, label);
+            __syncwarp();                        // lane 0 has the label's logit, which another lane may write over (dlogits in its place)
             if (a.dz) {
                 T* dr = static_cast<T*>(a.dz) + row * a.dz_stride - o;
                 const float f = label.has > 0 ? (r.empty ? 0.f : over) : label.has == 0 ? 0.f : nan_f(), g = f == 0.f ? 0.f : f / sums.s;

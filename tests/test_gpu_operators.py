@@ -415,6 +415,25 @@ def test_loss_logprob(case, dtype):
     zg()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape, shift", [((5000, 10), 0), ((3001, 33), 1), ((2000, 479), 0), ((700, 1000), 3), ((300, 2048), 0), ((90, 5003), 1),
+                                          ((9, 40001), 0), ((2, 21, 40, 50), 0), ((3, 70, 9, 9), 1), ((1, 700, 8, 6), 0)])
+def test_loss_and_delta_in_the_logits_place_in_one_call(shape, shift, dtype):
+    """The loss reads the label's logit where another thread writes its delta: the same bits as with a place for the delta."""
+    z = (3 * _normal(shape, 38)).to(dtype)
+    labels = torch.randint(0, shape[1], _rows_of(shape), generator=torch.Generator().manual_seed(8)).cuda()
+    zd, zg = guarded(z, 0, shift)
+    dz, dg = guarded(torch.zeros_like(z), 0, shift)
+    ws = torch.empty(ftp.ftp_loss_logprob_workspace_bytes(z), dtype=torch.uint8, device="cuda")
+    loss, want = torch.full((1,), GUARD, device="cuda"), torch.full((1,), GUARD, device="cuda")
+    ftp.ftp_loss_logprob(zd, labels, dz, want, ws, scale=64.0)
+    for _ in range(8):
+        zd.copy_(z)
+        ftp.ftp_loss_logprob(zd, labels, zd, loss, ws, scale=64.0)
+        assert torch.equal(loss, want) and torch.equal(zd, dz)
+    zg(), dg()
+
+
 def test_loss_without_a_labelled_row_and_with_ruled_out_ones():
     for shape in ((6, 50), (2, 5, 3, 3)):
         z = _normal(shape, 36).cuda()
