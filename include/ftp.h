@@ -512,7 +512,7 @@ int ftp_ckpt_load(const ftp_dims* d, const void* ckpt, void* x, long long x_stri
  * {n = N, c = C, p = H W} of the plan's input, any type at saving time) and lets the plans share one workspace.  Writes the
  * checkpoint's values to x (caller's device buffer, fp32, shape of the plan's input), runs ftp_forward on them (without output map)
  * and ftp_backward: dx and dparams are those of the plan at the values of the checkpoint.  Needs no preceding ftp_forward.
- * Arguments otherwise as for ftp_backward; dx must not be x.
+ * Arguments otherwise as for ftp_backward; neither dx nor dy may be x (FTP_ERR_ARG).
  */
 int ftp_backward_ckpt(ftp_plan* plan, const void* ckpt, float* x, const float* dy, const float* params, float* dx, float* dparams,
                       void* workspace, void* stream);

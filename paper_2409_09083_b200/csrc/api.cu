@@ -1097,7 +1097,7 @@ int ftp_backward(ftp_plan* plan, const float* x, const float* dy, const float* p
 int ftp_backward_ckpt(ftp_plan* plan, const void* ckpt, float* x, const float* dy, const float* params, float* dx, float* dparams,
                       void* workspace, void* stream)
 {
-    if (!plan || !ckpt || !x || dx == x || !dy || !params || !dparams || !workspace || !aligned256(workspace)) return FTP_ERR_ARG;
+    if (!plan || !ckpt || !x || dx == x || dy == x || !dy || !params || !dparams || !workspace || !aligned256(workspace)) return FTP_ERR_ARG;
     const MapShape& in = plan->maps.front();
     const ftp_dims d{(int)sizeof(ftp_dims), FTP_TYPE_F32, plan->N, in.C, (long long)in.H * in.W};
     int rc = ftp_ckpt_load(&d, ckpt, x, 0, stream);

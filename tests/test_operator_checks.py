@@ -201,3 +201,12 @@ def test_backward_ckpt_checks_its_sizes():
                 (h, SOME, SOME, SOME, SOME, None, None, SOME), (h, SOME, SOME, SOME, SOME, None, SOME, SOME + 8),
                 (h, SOME + 8, SOME, SOME, SOME, None, SOME, SOME)):
         assert lib.ftp_backward_ckpt(*bad, None) == ARG
+
+
+def test_backward_ckpt_refuses_a_delta_in_the_place_that_it_fills():
+    """x receives the checkpoint's values before the delta is read: where input and output maps have one size, they could be one array."""
+    from paper_2409_09083_b200 import synth
+    plan = ftp.ftp_plan([synth.conv(4, 4, 3)], 1, 4, 8, 8, (1, 1), ((1, 1),))
+    assert plan.in_floats == plan.out_floats
+    h, x = plan._h, SOME + (1 << 16)
+    assert lib.ftp_backward_ckpt(h, SOME, x, x, SOME, None, SOME, SOME, None) == ARG
