@@ -82,7 +82,7 @@ class Chain:
     @_on_its_device
     def forward(self, x, params, y=None, keep=False, stream=None):
         """Logits of the last plan ([N, classes, H, W]), in `y` or a buffer of the chain; keep: the checkpoints for a backward pass."""
-        self._check(x, params)
+        self._check(x, params, y=y)
         cur = x
         for i, plan in enumerate(self.plans):
             sl, last = self.slices[i], i + 1 == len(self.plans)
@@ -104,7 +104,7 @@ class Chain:
     @_on_its_device
     def step_grad(self, x, labels, params, dparams, loss_out, dx=None, stream=None):
         """Loss (mean over the labelled pixels of -log p) and gradient of one batch; labels: int64 [N, H, W] of the last map."""
-        self._check(x, params)
+        self._check(x, params, labels=labels, dparams=dparams, loss_out=loss_out, dx=dx)
         if dparams.numel() != self.param_floats:
             raise ValueError(f"dparams has {dparams.numel()} elements, the chain needs {self.param_floats}")
         last, ws = len(self.plans) - 1, self.workspace
@@ -135,13 +135,13 @@ class Chain:
         self.step_grad(x, labels, params, dparams, loss_out, dx=dx, stream=stream)
         ftp.ftp_sgd(params, dparams, lr, stream=stream)
 
-    def _check(self, x, params):
+    def _check(self, x, params, **others):
         if params.numel() != self.param_floats:
             raise ValueError(f"params has {params.numel()} elements, the chain needs {self.param_floats}")
         if x.numel() != self.plans[0].in_floats:
             raise ValueError(f"x has {x.numel()} elements, the chain needs {self.plans[0].in_floats}")
-        for t, name in ((x, "x"), (params, "params")):
-            if t.device != self.workspace.device:
+        for name, t in (("x", x), ("params", params), *others.items()):
+            if t is not None and t.device != self.workspace.device:
                 raise ValueError(f"{name} is on {t.device}, the chain on {self.workspace.device}")
 
 

@@ -221,3 +221,25 @@ def test_parameters_off_the_16_byte_grid_and_a_plan_in_two_places(precision):
     grad = torch.empty(again.param_floats, device="cuda")
     ftp.ftp_backward(again, cur, delta, part[0], None, grad, ws)
     assert torch.equal(grad, grads[0][chain.slices[2][0]]) and torch.equal(loss, losses[0])
+
+
+@pytest.mark.parametrize("name", ["dparams", "dx", "labels", "loss_out"])
+def test_what_a_step_writes_and_reads_is_on_the_chains_device(name):
+    plans = _plans()
+    chain = chains.Chain(plans, device="cpu")
+    x, params = torch.zeros(plans[0].in_floats), torch.zeros(chain.param_floats)
+    n, _, h, w = chain.shapes[-1]
+    given = dict(labels=torch.zeros((n, h, w), dtype=torch.int64), dparams=params.clone(), loss_out=torch.zeros(1), dx=x.clone())
+    given[name] = given[name].to("meta")
+    with pytest.raises(ValueError, match=f"{name} is on meta, the chain on cpu"):
+        chain.step_grad(x, params=params, **given)
+    with pytest.raises(ValueError, match=f"{name} is on meta, the chain on cpu"):
+        chain.step(x, params=params, lr=0.1, **given)
+
+
+def test_a_chains_output_is_on_its_device():
+    plans = _plans()
+    chain = chains.Chain(plans, device="cpu")
+    x, params = torch.zeros(plans[0].in_floats), torch.zeros(chain.param_floats)
+    with pytest.raises(ValueError, match="y is on meta, the chain on cpu"):
+        chain.forward(x, params, y=torch.empty(chain.shapes[-1], device="meta"))
