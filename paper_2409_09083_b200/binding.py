@@ -584,7 +584,10 @@ def ftp_backward_ckpt(plan, ckpt, x, dy, params, dx, dparams, workspace, stream=
                                   (params, "params", plan.param_floats), (dx, "dx", plan.in_floats, True),
                                   (dparams, "dparams", plan.param_floats))
     pk = _bytes(ckpt, "ckpt", ftp_ckpt_bytes(plan.shape), x.device)[0]
-    _check(_lib.ftp_backward_ckpt(plan._h, pk, px, pdy, pp, pdx, pg, ws.ptr, _stream(stream)))
+    for t, name in ((dy, "dy"), (params, "params"), (dx, "dx"), (dparams, "dparams"), (workspace, "workspace")):
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name} is on {t.device}, expected {x.device}")
+    _call(_lib.ftp_backward_ckpt, x, "x", stream, plan._h, pk, px, pdy, pp, pdx, pg, ws.ptr)
 
 
 def ftp_norm_forward(x, weight, bias, y, mean=None, rstd=None, eps=1e-5, ckpt=None, stream=None):

@@ -210,3 +210,46 @@ def test_backward_ckpt_refuses_a_delta_in_the_place_that_it_fills():
     assert plan.in_floats == plan.out_floats
     h, x = plan._h, SOME + (1 << 16)
     assert lib.ftp_backward_ckpt(h, SOME, x, x, SOME, None, SOME, SOME, None) == ARG
+
+
+class _OnGpu:
+    """A float32 tensor's outside, on a device that this machine need not have."""
+    dtype, is_cuda = torch.float32, True
+
+    def __init__(self, count, device):
+        self.count, self.device = count, torch.device(device)
+
+    def numel(self):
+        return self.count
+
+    def element_size(self):
+        return 4
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return SOME
+
+    def get_device(self):
+        return self.device.index
+
+
+def test_backward_ckpt_runs_on_its_arrays_device(monkeypatch):
+    """As the other operators do: with x's device current, on that device's stream, and not with arrays of several devices."""
+    from paper_2409_09083_b200 import synth
+    plan = ftp.ftp_plan([synth.conv(4, 8, 3)], 1, 4, 8, 8, (1, 1), ((1, 1),))
+    counts = dict(ckpt=ftp.ftp_ckpt_bytes(plan.shape), x=plan.in_floats, dy=plan.out_floats, params=plan.param_floats, dx=plan.in_floats,
+                  dparams=plan.param_floats, workspace=plan.workspace_bytes)
+    arrays = {k: _OnGpu(n, "cuda:1") for k, n in counts.items()}
+    seen = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: pytest.fail("the current device's stream was taken"))
+    monkeypatch.setattr(binding, "_call", lambda fn, x, name, stream, *args: seen.append((x, name, stream, args)))
+    ftp.ftp_backward_ckpt(plan, **arrays)
+    x, name, stream, args = seen[0]
+    assert x is arrays["x"] and name == "x" and stream is None
+    assert [getattr(a, "value", a) for a in args] == [plan._h.value] + 7 * [SOME]
+    for k in counts:
+        if k != "x":
+            with pytest.raises(ValueError, match=f"{k} (is|must be a contiguous tensor) on cuda:"):
+                ftp.ftp_backward_ckpt(plan, **{**arrays, k: _OnGpu(counts[k], "cuda:0")})
