@@ -524,7 +524,8 @@ __device__ __forceinline__ Tile tile_of(const NormArgs& a, const Walk& w, int pi
     return t;
 }
 
-// Adds K values of each pixel over the `share` warps of the block, in their order (1: the warp's own).
+// Adds K values of each pixel over the `share` warps of the block, in their order (1: the warp's own).  A block's last warp may have fewer
+// channels and come here by another branch than the others, where __syncthreads() would have to be one place of the program for all.
 template <int K, int V> __device__ __forceinline__ void pixel_sum(Vals<V> (&v)[K], int share, float* red)
 {
     if (share == 1) return;
@@ -533,7 +534,7 @@ template <int K, int V> __device__ __forceinline__ void pixel_sum(Vals<V> (&v)[K
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int j = 0; j < V; ++j) red[((warp * K + k) * V + j) * 32 + lane] = v[k].v[j];
-    __syncthreads();
+    block_barrier();
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] = all<V>(0.f);
 #pragma unroll 4

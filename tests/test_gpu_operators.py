@@ -129,6 +129,20 @@ def test_norm_backward(case, from_ckpt, dtype):
     dyg()
 
 
+# maps of a whole tile and a part of one, whose channels leave the last warp of a block fewer than the others have (from 15 channels in
+# two warps to 1000 in 32)
+UNEVEN = [((1, 15, 11, 12), 0, 0), ((2, 31, 7, 10), 0, 0), ((1, 60, 11, 12), 0, 0), ((2, 125, 7, 10), 0, 0), ((2, 250, 7, 10), 0, 0),
+          ((2, 500, 7, 10), 0, 0), ((2, 500, 7, 10), 2, 1), ((1, 1000, 7, 10), 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", UNEVEN, ids=_ids)
+def test_norm_of_maps_whose_last_warp_has_fewer_channels(case, dtype):
+    test_norm_forward(case, dtype)
+    for from_ckpt in (False, True):
+        test_norm_backward(case, from_ckpt, dtype)
+
+
 @pytest.mark.parametrize("shape", [(6, 40), (2, 6, 5, 3)])
 def test_norm_gradients_against_differences(shape):
     """dx, dweight and dbias against central differences of sum(y t) of the plain forward pass in 64 bits."""
