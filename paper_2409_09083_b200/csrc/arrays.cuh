@@ -525,6 +525,12 @@ template <auto K> inline int resident(int threads, size_t smem)
     return n < 1 ? 1 : n > 32 ? 32 : n;
 }
 inline int launched() { return cudaGetLastError() == cudaSuccess ? FTP_OK : FTP_ERR_CUDA; }
+// A runtime call was refused: the error that it left with the thread is this call's, not the next one's.
+inline int refused()
+{
+    cudaGetLastError();
+    return FTP_ERR_CUDA;
+}
 
 }  // namespace arr
 }  // namespace ftp

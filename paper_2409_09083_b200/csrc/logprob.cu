@@ -1061,7 +1061,7 @@ template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(co
             int n = 0;
             if (!allow_smem(kernel, ring, kRingBytes) ||
                 (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
-                cudaOccupancyMaxActiveClusters(&n, kernel, &ask) != cudaSuccess || n < 1) return FTP_ERR_CUDA;
+                cudaOccupancyMaxActiveClusters(&n, kernel, &ask) != cudaSuccess || n < 1) return refused();
             at.store(n, std::memory_order_relaxed);
         }
         slots = at.load(std::memory_order_relaxed);
@@ -1079,8 +1079,8 @@ template <class T, bool SHIFT, int MODE, int TH, bool FIN> int run_block_rows(co
     cfg.gridDim = dim3(*blocks); cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (!allow_smem(kernel, smem, kRingBytes) ||
-        (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) return FTP_ERR_CUDA;
-    if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, share * (int)(16 / sizeof(T)), stages, dz_vec) != cudaSuccess) return FTP_ERR_CUDA;
+        (cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)) return refused();
+    if (cudaLaunchKernelEx(&cfg, kernel, a, cluster, share * (int)(16 / sizeof(T)), stages, dz_vec) != cudaSuccess) return refused();
     return launched();
 }
 // A cluster shares a row that is longer than a stage, or that few rows leave to few blocks; rows of up to 16 KB take 128 threads.
@@ -1285,7 +1285,7 @@ int ftp_loss_logprob(const ftp_dims* d, const void* logits, long long logits_str
     if ((rows > 0 && !dlogits && !loss_out) || !(scale >= -3.0e38f && scale <= 3.0e38f) || !aligned(loss_out, 4)) return FTP_ERR_ARG;
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < kLossWorkspace) return FTP_ERR_ARG;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (rows == 0) return !loss_out || cudaMemsetAsync(loss_out, 0, 4, st) == cudaSuccess ? FTP_OK : FTP_ERR_CUDA;
+    if (rows == 0) return !loss_out || cudaMemsetAsync(loss_out, 0, 4, st) == cudaSuccess ? FTP_OK : refused();
     const size_t size = type_size(d->type);
     if (!logits || !labels || !aligned(logits, size) || !aligned(dlogits, size) || !aligned(labels, 8)) return FTP_ERR_ARG;
     if (!fix_stride(d, &logits_stride) || (dlogits && !fix_stride(d, &dlogits_stride))) return FTP_ERR_ARG;

@@ -983,7 +983,7 @@ template <class T, int V, int VPT, int FORM, bool CK> int run_bwd_rows(const Nor
     // rows of a group a multiple of V rows apart (unless each has one row only)
     if (FORM == kShift && (long long)blocks * per < a.rows)
         while ((blocks * per) % V) --blocks;
-    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, smem, (size_t)512 * VPT * V * 4)) return FTP_ERR_CUDA;
+    if (!allow_smem(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, smem, (size_t)512 * VPT * V * 4)) return refused();
     launch(norm_bwd_rows_kernel<T, V, VPT, FORM, CK>, dim3(blocks), dim3(threads), smem, ls, a, tpr);
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
@@ -1176,7 +1176,7 @@ int ftp_norm_backward(const ftp_dims* d, const void* x, long long x_stride, cons
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (rows == 0) {                                     // sums over nothing
         if (dweight && (cudaMemsetAsync(dweight, 0, (size_t)d->c * 4, st) != cudaSuccess ||
-                        cudaMemsetAsync(dbias, 0, (size_t)d->c * 4, st) != cudaSuccess)) return FTP_ERR_CUDA;
+                        cudaMemsetAsync(dbias, 0, (size_t)d->c * 4, st) != cudaSuccess)) return refused();
         return FTP_OK;
     }
     if ((x == nullptr) == (ckpt == nullptr) || !dy || !mean || !rstd) return FTP_ERR_ARG;

@@ -752,3 +752,49 @@ def test_two_host_threads_call_one_kernel_with_much_and_little_shared_memory(mak
     assert refused == [0, 0], refused
     for (out, _), first in zip(results, want):
         assert all(torch.equal(a, b) for a, b in zip(out, first))
+
+
+def test_a_refused_call_leaves_no_error_for_the_next_one():
+    """The default stream takes nothing while another one is captured (in the mode that forbids it), and the capture is lost; the calls that
+    follow are good ones.  In a process of its own, for the lost capture's sake."""
+    code = """
+import ctypes
+import torch
+import paper_2409_09083_b200 as ftp
+z = torch.randn((90, 40001), device="cuda")
+labels = torch.zeros(90, dtype=torch.int64, device="cuda")
+dz, loss, none = torch.empty_like(z), torch.empty(1, device="cuda"), torch.empty((0, 40001), device="cuda")
+lws = torch.empty(ftp.ftp_loss_logprob_workspace_bytes(z), dtype=torch.uint8, device="cuda")
+nws = torch.empty(ftp.ftp_norm_workspace_bytes(z), dtype=torch.uint8, device="cuda")
+dw, db, stat = torch.empty(40001, device="cuda"), torch.empty(40001, device="cuda"), torch.empty(0, device="cuda")
+x, back = torch.randn((40, 70), device="cuda"), torch.empty((40, 70), device="cuda")
+ckpt = torch.empty(ftp.ftp_ckpt_bytes(x), dtype=torch.uint8, device="cuda")
+calls = [lambda: ftp.ftp_loss_logprob(z, labels, dz, loss, lws), lambda: ftp.ftp_loss_logprob(none, labels[:0], none, loss, lws),
+         lambda: ftp.ftp_norm_backward(none, none, None, stat, stat, None, dw, db, nws)]
+for call in calls:
+    call()
+torch.cuda.synchronize()
+for call in calls:
+    graph, handle = torch.cuda.CUDAGraph(), ctypes.c_void_p()
+    torch.cuda.cudart().cudaStreamCreate(ctypes.addressof(handle))            # (torch's own do not stand back behind the default stream)
+    side = torch.cuda.ExternalStream(handle.value)
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+    try:
+        call()
+        raise SystemExit("the call was not refused")
+    except ftp.FtpError:
+        pass
+    with torch.cuda.stream(side):
+        try:
+            graph.capture_end()
+        except RuntimeError:
+            pass
+    ftp.ftp_ckpt_save(x, ckpt)
+    ftp.ftp_ckpt_load(ckpt, back)
+    call()
+    torch.cuda.synchronize()
+    assert (back - x).abs().max() <= x.abs().max() / 127
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=pathlib.Path(__file__).resolve().parents[1], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
