@@ -143,6 +143,20 @@ def test_norm_of_maps_whose_last_warp_has_fewer_channels(case, dtype):
         test_norm_backward(case, from_ckpt, dtype)
 
 
+# two pixels a lane in 16 bits with more than 128 channels, and maps of 513 to 1024 channels, which the forward pass gives to a block
+# of up to 32 warps
+WIDE = [((3, 160, 7, 10), 0, 0), ((2, 300, 7, 10), 0, 0), ((1, 512, 7, 10), 4, 2), ((1, 640, 9, 9), 3, 1), ((1, 700, 7, 10), 0, 0), ((1, 1024, 6, 12), 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", WIDE, ids=_ids)
+def test_norm_of_maps_of_many_channels(case, dtype):
+    test_norm_forward(case, dtype)
+    for from_ckpt in (False, True):
+        test_norm_backward(case, from_ckpt, dtype)
+    test_ckpt_is_defined_to_the_bit(case, dtype)
+
+
 @pytest.mark.parametrize("shape", [(6, 40), (2, 6, 5, 3)])
 def test_norm_gradients_against_differences(shape):
     """dx, dweight and dbias against central differences of sum(y t) of the plain forward pass in 64 bits."""
@@ -584,6 +598,41 @@ def test_arrays_of_different_alignment(shape, dtype):
     assert abs(got["loss"].item() - dense["loss"].item()) <= 1e-5 * (1 + abs(dense["loss"].item()))
     for check in (xg, dyg, yg, dxg, dzg, dz2g):
         check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(6, 372), (40, 1111), (3, 5001), (2, 9001), (700, 33), (2, 40, 10, 6), (3, 33, 5, 7)])
+def test_column_sums_and_loss_of_arrays_of_different_alignment(shape, dtype):
+    """Every array another distance off the 16-byte grid: each column's sums to the rounding of its own terms, the loss to that of its rows."""
+    x, dy, w = _normal(shape, 63, dtype), _normal(shape, 64, dtype), _normal(shape[1:2], 65)
+    labels = torch.randint(-1, shape[1], _rows_of(shape), generator=torch.Generator().manual_seed(4))
+    _, m, r = norm_forward(x, w, None, EPS)
+    mean, rstd = m.float().cuda(), r.float().cuda()
+    n = labels.numel()
+    want, d, p = logprob(x, labels, 1)
+    known = labels.reshape(-1) >= 0
+    count = max(1, int(known.sum()))
+    hit = torch.arange(shape[1])[None] == labels.reshape(-1, 1)
+    for (px, sx), (py, sy), (po, so) in (((3, 1), (6, 2), (5, 0)), ((0, 0), (1, 3), (2, 6)), ((2, 5), (0, 0), (0, 1)), ((1, 7), (8, 7), (3, 4))):
+        (xd, xg), (dyd, dyg), (dx, dxg) = guarded(x, px, sx), guarded(dy, py, sy), guarded(torch.zeros_like(x), po, so)
+        dw, db, loss = torch.full(shape[1:2], GUARD, device="cuda"), torch.full(shape[1:2], GUARD, device="cuda"), torch.full((1,), GUARD, device="cuda")
+        ws = torch.full((ftp.ftp_norm_workspace_bytes(x),), 255, dtype=torch.uint8, device="cuda")
+        ftp.ftp_norm_backward(xd, dyd, w.cuda(), mean, rstd, dx, dw, db, ws)
+        dx64, dw64, db64, dx_size, dw_size, db_size = norm_backward(x, dy, w, mean, rstd)
+        # (the bounds of the aligned arrays: row sums in trees, at most one thread adds all rows of a column in turn)
+        close(rows(dx), dx64, HALF_STEP[dtype] * dx64.abs() + TINY[dtype] + 64 * U * dx_size, "dx")
+        close(dw, dw64, (n + 32) * U * dw_size, "dweight")
+        close(db, db64, (n + 32) * U * db_size, "dbias")
+        lws = torch.full((ftp.ftp_loss_logprob_workspace_bytes(x),), 255, dtype=torch.uint8, device="cuda")
+        dz, dzg = guarded(torch.zeros_like(x), po, so)
+        ftp.ftp_loss_logprob(xd, labels.cuda(), dz, loss, lws)
+        want_d = torch.where(known[:, None], (p - hit.double()) / count, 0.0)
+        bound = HALF_STEP[dtype] * want_d.abs() + TINY[dtype] + U * (64 + 4 * d.abs()) * (p + hit) * known[:, None] / count + 2.0 ** -140
+        close(rows(dz), want_d, bound, "dlogits")
+        terms = want["logp"][known].abs().sum() / count
+        close(loss[0], -want["logp"][known].sum() / count, (128 + 16 + n) * U * (terms + 1), "loss")
+        for check in (xg, dyg, dxg, dzg):
+            check()
 
 
 def test_offsets_past_32_bits():
