@@ -243,3 +243,21 @@ def test_a_chains_output_is_on_its_device():
     x, params = torch.zeros(plans[0].in_floats), torch.zeros(chain.param_floats)
     with pytest.raises(ValueError, match="y is on meta, the chain on cpu"):
         chain.forward(x, params, y=torch.empty(chain.shapes[-1], device="meta"))
+
+
+@pytest.mark.gpu
+def test_a_chain_on_a_stream_that_is_given():
+    x, params, labels = (t.cuda() for t in _batch(chains.Chain(_plans()), 5))
+    results = []
+    for stream in (None, torch.cuda.Stream()):
+        chain = chains.Chain(_plans())
+        p, dparams, loss = params.clone(), torch.empty_like(params), torch.empty(1, device="cuda")
+        s = chain.shapes[-1]
+        tl, ti = torch.empty((s[0], 2) + s[2:], device="cuda"), torch.empty((s[0], 2) + s[2:], dtype=torch.int64, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(2):
+            chain.step(x, labels, p, dparams, 0.02, loss, stream=stream)
+        chain.answer(x, p, tl, ti, stream=stream)
+        torch.cuda.synchronize()
+        results.append((p, dparams, loss, tl, ti))
+    assert all(torch.equal(a, b) for a, b in zip(*results))

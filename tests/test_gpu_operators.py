@@ -157,6 +157,34 @@ def test_norm_of_maps_of_many_channels(case, dtype):
     test_ckpt_is_defined_to_the_bit(case, dtype)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", SHAPES + UNEVEN + WIDE, ids=_ids)
+def test_norm_backward_in_the_place_of_x(case, dtype):
+    """dx written over x: the same bits as in a place of its own, in each form of the kernel."""
+    shape, pad, shift = case
+    x, dy, w = _normal(shape, 13, dtype), _normal(shape, 14, dtype), _normal(shape[1:2], 15).cuda()
+    (xd, xg), (dyd, _), (dx, _) = guarded(x, pad, shift), guarded(dy, pad, shift), guarded(torch.zeros_like(x), pad, shift)
+    _, m, r = norm_forward(x, w, None, EPS)
+    ws = torch.empty(ftp.ftp_norm_workspace_bytes(x), dtype=torch.uint8, device="cuda")
+    sums = [torch.empty_like(w) for _ in range(4)]
+    for to, dw, db in ((dx, *sums[:2]), (xd, *sums[2:])):
+        ftp.ftp_norm_backward(xd, dyd, w, m.float().cuda(), r.float().cuda(), to, dw, db, ws)
+    assert torch.equal(xd, dx) and torch.equal(sums[0], sums[2]) and torch.equal(sums[1], sums[3])
+    xg()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("case", [((7, 65, 1, 1), 3, 1), ((300, 24, 1, 1), 0, 0)], ids=_ids)
+def test_maps_of_one_pixel_are_rows(case, dtype):
+    test_norm_forward(case, dtype)
+    for from_ckpt in (False, True):
+        test_norm_backward(case, from_ckpt, dtype)
+    test_ckpt_is_defined_to_the_bit(case, dtype)
+    test_logprob(case, dtype)
+    test_logprob_backward(case, dtype)
+    test_loss_logprob(case, dtype)
+
+
 @pytest.mark.parametrize("shape", [(6, 40), (2, 6, 5, 3)])
 def test_norm_gradients_against_differences(shape):
     """dx, dweight and dbias against central differences of sum(y t) of the plain forward pass in 64 bits."""
@@ -847,3 +875,31 @@ for call in calls:
 """
     done = subprocess.run([sys.executable, "-c", code], cwd=pathlib.Path(__file__).resolve().parents[1], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_one_dimension_is_one_row_and_the_stream_may_be_given():
+    """x of shape [c], on a stream that is not the current one, given as an object and as its handle: the bits of the [1, c] call."""
+    c = 1234
+    x, dy, w = _normal((1, c), 100).cuda(), _normal((1, c), 101).cuda(), _normal((c,), 102).cuda()
+    labels = torch.tensor([77], device="cuda")
+    side = torch.cuda.Stream()
+
+    def everything(x, dy, top, **on):
+        new = lambda n, dtype=torch.float32: torch.full((n,), 3, dtype=dtype, device="cuda")            # noqa: E731
+        y, dx, dz, dz2, back = (torch.empty_like(x) for _ in range(5))
+        mean, rstd, logp, lse, h, loss, dw, db = new(1), new(1), new(1), new(1), new(1), new(1), new(c), new(c)
+        tl, ti = torch.empty(top, device="cuda"), torch.empty(top, dtype=torch.int64, device="cuda")
+        ckpt, nws, lws = (new(n, torch.uint8) for n in (ftp.ftp_ckpt_bytes(x), ftp.ftp_norm_workspace_bytes(x), ftp.ftp_loss_logprob_workspace_bytes(x)))
+        torch.cuda.synchronize()
+        ftp.ftp_norm_forward(x, w, w, y, mean, rstd, ckpt=ckpt, **on)
+        ftp.ftp_norm_backward(None, dy, w, mean, rstd, dx, dw, db, nws, ckpt=ckpt, **on)
+        ftp.ftp_ckpt_save(y, ckpt, **on)
+        ftp.ftp_ckpt_load(ckpt, back, **on)
+        ftp.ftp_logprob(y, labels, logp, lse, h, tl, ti, **on)
+        ftp.ftp_logprob_backward(y, labels, lse, h, logp, rstd, dz, **on)
+        ftp.ftp_loss_logprob(y, labels, dz2, loss, lws, **on)
+        torch.cuda.synchronize()
+        return [t.flatten() for t in (y, mean, rstd, ckpt, dx, dw, db, back, logp, lse, h, tl, ti, dz, loss, dz2)]
+    want = everything(x, dy, (1, 4))
+    for on in (dict(stream=side), dict(stream=side.cuda_stream)):
+        assert all(torch.equal(a, b) for a, b in zip(everything(x[0], dy[0], (4,), **on), want))
