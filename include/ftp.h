@@ -563,7 +563,7 @@ int ftp_logprob(const ftp_dims* d, const void* logits, long long logits_stride, 
  * Gradient of the above: for deltas dlogp and dentropy of each row (device, n p floats, each may be NULL: 0)
  *   dlogits = dlogp (1[class = label] - p) - dentropy p (log p + entropy),
  * with the lse and entropy (NULL if dentropy is) that ftp_logprob gave.  Rows without a label take dlogp = 0; a label of c or more
- * makes its row NaN; a row whose classes are all ruled out gets 0.  dlogits may be logits.
+ * makes its row NaN; a row whose classes are all ruled out gets 0, whatever its label.  dlogits may be logits.
  */
 int ftp_logprob_backward(const ftp_dims* d, const void* logits, long long logits_stride, const long long* labels,
                          const float* lse, const float* entropy, const float* dlogp, const float* dentropy,
@@ -571,8 +571,9 @@ int ftp_logprob_backward(const ftp_dims* d, const void* logits, long long logits
 
 /*
  * Loss over class labels, beside ftp_loss_mse: L = -(1/M) sum of logp over the M rows that have a label (0 if M = 0), and
- * dlogits = scale dL/dlogits = (scale / M) (p - 1[class = label]), 0 in rows without a label and in rows whose classes are all ruled out.  `scale` keeps deltas of 16
- * bits in range (1: none); L is not scaled.  dlogits may be NULL and may be logits; loss_out (device, 1 float) may be NULL; not both.
+ * dlogits = scale dL/dlogits = (scale / M) (p - 1[class = label]), 0 in rows without a label and in rows whose classes are all ruled out.  A label
+ * of c or more counts as one and makes L and its row NaN.  `scale` keeps deltas of 16 bits in range (1: none); L is not scaled.
+ * dlogits may be NULL and may be logits; loss_out (device, 1 float) may be NULL; not both.
  * One pass over the logits.  n p < 2^31 (else FTP_ERR_TOO_LARGE).  workspace: device, 16-byte aligned, at least the size ftp_loss_logprob_workspace reports.
  */
 int ftp_loss_logprob_workspace(const ftp_dims* d, size_t* bytes);

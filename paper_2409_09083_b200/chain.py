@@ -12,6 +12,9 @@ share ONE workspace, and what outlives a plan's forward pass is the joint behind
 So the forward pass, the loss and the last plan's gradients are those of the network itself; the gradients before the last joint are
 taken at maps that are off by at most 1/127 of the largest magnitude among 32 neighbours.
 
+A joint is kept twice, as what its norm got and as what the next plan got.  A chain has one workspace and one set of maps and checkpoints:
+its calls follow one another on one stream, or one after the other by the caller's care; two streams at once want two chains.
+
 Parameters are one flat vector: plan 0, weight and bias of the norm behind it, plan 1, ...
 """
 import functools

@@ -7,7 +7,8 @@
 //
 // The best classes come without sorting: a row is cut into 32 parts, and the top-th largest of the parts' maxima is a
 // bound that at least `top` values reach and few more do (for 8 of 32 parts about 9).  Those are collected in shared memory and
-// each finds its own place by counting the better ones.  Where equal values overflow the list, the places are found one by one.
+// each finds its own place by counting the better ones.  Where equal values overflow the list, the places are found one by one, each in a
+// reading of the whole row: right, but slow (8 best of 4096 x 32000 bf16: 68 us of normal values, 1390 of equal ones).
 // A value and its class make one 64-bit key whose order is descending value, then ascending class.
 #include <cooperative_groups.h>
 
@@ -171,7 +172,8 @@ __device__ __forceinline__ unsigned order_of(float v)
     const unsigned b = __float_as_uint(v + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-// A bound that `top` of the 32 lanes' values reach at least: the maximum, taken away `top` - 1 times with all that are equal to it.
+// A bound that `top` of the 32 lanes' values reach at least: the maximum, taken away `top` - 1 times with all that are equal to it.  (Equal
+// ones count as one, so that the bound is lower than it need be where maxima tie, as those of 16 bits often do.)
 __device__ __forceinline__ float bound_of(float v, int top)
 {
     unsigned mine = order_of(v), best = 0;
@@ -652,7 +654,8 @@ logprob_block_rows_kernel(LpArgs a, int cluster, int part, int stages, bool dz_v
             }
             if (t == 0) sh.whole[turn] = sums;
             // one barrier a row: what is read here is written again for the row after the next, behind the next row's barrier (300 bf16
-            // rows of 250000 classes: 102 us; with a second barrier and each thread joining all blocks' sums one after the other 140)
+            // rows of 250000 classes without best ones: 102 us; with a second barrier and each thread joining all blocks' sums one after the other
+            // 140)
             cl.sync();
             if (MODE == kLoss || rank == 0) sums = join_lanes(*cl.map_shared_rank(&sh.whole[turn], lane & (cluster - 1)), cluster);
             if (want_top && rank == 0) {
@@ -809,6 +812,7 @@ __device__ __forceinline__ void logprob_tile(const LpArgs& a, long long n, int p
         for (int j = 0; j < V; ++j) write_stats(a, row + j, r[j], label[j]);
     }
     if constexpr (TOP) {
+        // Every place looks at every class (8 x 21 x 416 x 416: 34 us without best classes, 57 with one, 120 with 5, 359 with 20).
         unsigned long long before = ~0ull;
         for (int k = 0; k < a.top; ++k) {
             unsigned long long best = 0;
@@ -1096,7 +1100,8 @@ template <class T, bool SHIFT, int MODE> int pick_block_rows(const LpArgs& a, bo
     if constexpr (MODE == kStats) {
         // a warp a row from 8 rows an SM on, and from 3 on where a row would take a cluster (us with 8 best classes, warps against
         // blocks: bf16 1200 rows of 16000 21 against 30, f32 1200 of 5000 13 against 20, f16 1200 of 32000 42 against 40, bf16 1000 of
-        // 32000 37 against 33; against clusters: 900 of 50000 54 against 89, f32 600 of 120000 208 against 266, 300 of them 200 against 136)
+        // 32000 37 against 33; against clusters: 900 of 50000 54 against 89, f32 600 of 120000 208 against 266, 300 of them 200 against 136).
+        // (Near 8 rows an SM the rule is up to 5 % on the slower side, as for the f16 rows above.)
         if (a.rows >= (cluster > 1 ? 3 : 8) * kSms) {
             const int fit = resident<logprob_stream_rows_kernel<T, SHIFT>>(kStreamWarps * 32, 0);
             const long long want = (a.rows + kStreamWarps - 1) / kStreamWarps, most = (long long)kSms * fit;

@@ -463,7 +463,8 @@ __global__ void __launch_bounds__(512, 1) norm_bwd_rows_kernel(NormArgs a, int t
     }
 }
 
-// Rows longer than that: two passes, the column sums of the block in its partial set itself (a thread's own columns).
+// Rows longer than that: two passes, the column sums of the block in its partial set itself (a thread's own columns), read and written for every
+// row: 1000 x 12000 fp32 takes 82 us, 22 of which are its bytes once.
 template <class T, bool CK> __global__ void __launch_bounds__(1024) norm_bwd_long_rows_kernel(NormArgs a)
 {
     __shared__ float red[2][64];
@@ -988,7 +989,8 @@ template <class T, int V, int VPT, int FORM, bool CK> int run_bwd_rows(const Nor
     return sum_sets(a, blocks, dweight, dbias, ls);
 }
 // 16 values to a thread (8 in fp32, whose values as read take the registers of two); rows of up to 8192 columns.  32 values of 16 bits
-// up to 16384: 2020 fp16 rows of 15353, forward and backward with a checkpoint, take 312 us, and 356 with rows read twice.
+// up to 16384, though they spill 736 to 1328 bytes a thread: 2020 fp16 rows of 15353, forward and backward with a checkpoint, take 312 us, and 356
+// with rows read twice.
 template <class T, int V, int FORM, bool CK> int pick_bwd_rows(const NormArgs& a, float* dweight, float* dbias, LaunchStream ls)
 {
     const long long vecs = (a.c + (FORM == kShift ? V - 1 : 0) + V - 1) / V;
@@ -1052,7 +1054,9 @@ template <class T, int V, bool CK> int fwd_map(const NormArgs& a, LaunchStream l
         return launched();                                                                                                                  \
     } while (0)
     // 16 warps an SM with 32 loads each on their way: with 20 and 24 the map of 16 x 32 x 304 x 304 takes 72 and 74 us instead of 64.  With
-    // a checkpoint to write the kernel is closer to the issue rate and takes all it can get (123 us with 16 warps, 111 with 24).
+    // a checkpoint to write the kernel is closer to the issue rate and takes all it can get (123 us with 16 warps, 111 with 24).  (Both measured on
+    // fp32 maps.)  More than 512 channels take blocks of 1024 threads, whose 64 registers spill with 32 channels a thread and a checkpoint (180
+    // bytes; 460 with two 16-bit pixels: 8 x 700 x 52 x 52 bf16 27 us, 45 with a checkpoint).
     const int cap = CK ? 32 : 16 / m.warps > 0 ? 16 / m.warps : 1;
     if (m.per <= 8 && m.warps <= 8) GO(norm_fwd_map_kernel<T, V, 8, CK, 256>);
     if constexpr (V == 4) GO(norm_fwd_map_kernel<T, V, 8, CK, 512>);
@@ -1073,6 +1077,8 @@ template <class T, int V, bool CK> int bwd_map(const NormArgs& a, float* dweight
             launch(norm_bwd_long_map_kernel<T, V, CK>, dim3(blocks), dim3(512 / V), 0, ls, a, (int)tiles);
             return sum_sets(a, blocks, dweight, dbias, ls);
         }
+    // (Two 16-bit pixels with 16 and 32 channels a thread spill 390 to 740 bytes: 8 x 64 x 208 x 208 bf16 48 us, f32 50; 8 x 512 x 104 x 104 bf16
+    // 98 us, f32 129, with twice the bytes to move.)
     const MapShapeOf m = map_shape(a.c, V == 4 ? 8 : CK && V == 2 && a.c <= 128 ? 8 : a.c <= 256 ? 16 : 32);
     const size_t smem = (size_t)a.c * 8 + 4 * (size_t)m.warps * 32 * V * 4;
     const long long want = (all + m.warps / m.share - 1) / (m.warps / m.share);

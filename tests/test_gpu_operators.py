@@ -903,3 +903,20 @@ def test_one_dimension_is_one_row_and_the_stream_may_be_given():
     want = everything(x, dy, (1, 4))
     for on in (dict(stream=side), dict(stream=side.cuda_stream)):
         assert all(torch.equal(a, b) for a, b in zip(everything(x[0], dy[0], (4,), **on), want))
+
+
+@pytest.mark.parametrize("shape", [(6, 50), (5, 3001), (2, 9, 5, 3)])
+def test_gradient_of_a_row_with_nothing_left_is_zero_whatever_its_label(shape):
+    z = _normal(shape, 110)
+    r = z.movedim(1, -1).reshape(-1, shape[1]).clone()
+    r[:3] = -float("inf")
+    z = like(r, shape).contiguous().cuda()
+    labels = torch.zeros(r.shape[0], dtype=torch.int64)
+    labels[1], labels[2], labels[4] = -1, shape[1], shape[1] + 7
+    labels = labels.reshape(_rows_of(shape)).cuda()
+    lse, h = torch.empty(_rows_of(shape), device="cuda"), torch.empty(_rows_of(shape), device="cuda")
+    ftp.ftp_logprob(z, None, lse=lse, entropy=h)
+    dz = torch.full(shape, GUARD, device="cuda")
+    ftp.ftp_logprob_backward(z, labels, lse, h, torch.ones_like(lse), torch.ones_like(lse), dz)
+    d = rows(dz)
+    assert not d[:3].any() and torch.isnan(d[4]).all() and torch.isfinite(d[torch.arange(len(d)) != 4]).all()
